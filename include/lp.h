@@ -362,6 +362,57 @@ int lp_conv2d(int op, int dtype, int impl, int N, int H, int W, int Cin, int Cou
 int lp_conv2d_fwd_noalloc(int N, int H, int W, int Cin, int Cout, int R, int stride, int pad, const void* x,
                           const float* w, void* y, void* stream);
 
+/*
+ * Operators at the end of a training step, on caller buffers.  (The paper's networks end in a linear layer and its updates are
+ * plain SGD, Eq. Parallel-ResNet-Backpropagation; these are the same two places for heads of many classes and for an update
+ * that is orthogonalised.)  dtype is LP_F32 or LP_BF16 and names the type of every tensor that is not said to be something
+ * else; matrices are contiguous, row by row, of any size; pointers are 16-byte aligned.  Calls are asynchronous on `stream`, on
+ * the current device, and may be recorded into a CUDA graph once a call of the kind has run outside a recording.  Each call
+ * needs a scratch buffer of its own while it runs (256-byte aligned, at least as many bytes as the ..._scratch_bytes call says;
+ * those return 0 for sizes that the operator refuses); it keeps nothing there between calls but the error word that
+ * lp_scratch_status reads.  Sums are taken in fp32 or more and in an order that depends on the sizes alone: the same call gives
+ * the same bits.
+ */
+
+/* Softmax cross entropy of a linear layer over V classes, without storing the logits:
+ *   l = x w^T + bias;  row_loss[t] = log sum_v exp l[t][v] - l[t][labels[t]];  loss = mean of row_loss over the counted rows
+ * A row counts if its label is a class, 0 <= labels[t] < V; any other label leaves the row out: its row_loss and its row of dx
+ * are 0 and nothing of x[t] (which may hold anything, NaN included) reaches dw or dbias.
+ *   x [T][D], w [V][D], bias [V] or NULL (entries may be -inf: that class then has probability 0), labels int32 [T]
+ *   loss_out: float[2] = { loss (0 if no row counts), number of counted rows }; row_loss: float[T] or NULL
+ *   dx [T][D], dw [V][D], dbias [V]: grad_scale times the gradient of loss, any of them NULL; overwritten.  All NULL: the loss
+ *     alone.
+ * In LP_F32 products are taken from 22 bits of each operand, relative to the largest magnitude of the tensor.  A row whose
+ * logits are all -inf has a loss and gradients of NaN, as the formula does.  The inputs are not changed; outputs must not
+ * overlap inputs.  The gradients take the rows in pieces whose exponentials fit 512 MB (256 rows at least). */
+size_t lp_linear_cross_entropy_scratch_bytes(int dtype, int T, int D, int V, int grads);
+int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const void* w, const void* bias,
+                            const int32_t* labels, float grad_scale, float* loss_out, float* row_loss, void* dx, void* dw,
+                            void* dbias, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Orthogonalisation by Newton-Schulz products, of `batch` matrices G [rows][cols] one after another in memory:
+ *   X = G / max(|G|_F, eps);  `steps` times  X <- a X + b (X X^T) X + c (X X^T)^2 X;  out = X
+ * coeffs: host float[3] = { a, b, c }, or NULL for { 3.4445, -4.7750, 2.0315 }, which take the singular values near 1 in five
+ * steps.  out may be g.  1 <= steps <= 32, eps >= 1e-30; coefficients under which a singular value of X passes 15, or one of
+ * b X X^T + c (X X^T)^2 passes 60, overflow.  A matrix that holds NaN or an infinity becomes NaN, no other matrix does.
+ * LP_BF16: iterates are kept in fp16 (11 significant bits, the first ones in two parts), the result is off by about half of
+ * bf16's own step.  LP_F32: every operand is kept in two parts. */
+size_t lp_orthogonalize_scratch_bytes(int dtype, int batch, int rows, int cols);
+int lp_orthogonalize(int dtype, int batch, int rows, int cols, const void* g, void* out, int steps, const float* coeffs,
+                     float eps, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The update with it, in place:  m <- momentum m + g;  u = nesterov ? g + momentum m : m;  O = orthogonalised u;
+ *   w <- (1 - lr weight_decay) w - lr scale O
+ * w, g in dtype, momentum_buf fp32, all [batch][rows][cols]; w, g and momentum_buf must not overlap.  `scale` is the caller's
+ * (for instance sqrt(max(1, rows / cols))).  Scratch, steps, coeffs, eps as in lp_orthogonalize. */
+int lp_muon_update(int dtype, int batch, int rows, int cols, void* w, const void* g, float* momentum_buf, float lr,
+                   float momentum, int nesterov, float weight_decay, float scale, int steps, const float* coeffs, float eps,
+                   void* scratch, size_t scratch_bytes, void* stream);
+
+/* Synchronise `stream` and return LP_OK, or LP_ERR_DEVICE_TIMEOUT if a bounded wait of the last of these operators that used
+ * `scratch` ran out (its results are then undefined). */
+int lp_scratch_status(const void* scratch, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

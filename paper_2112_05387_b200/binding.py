@@ -14,6 +14,8 @@ __all__ = [
     "lp_last_device_status", "lp_launch_count", "lp_conv_profile", "lp_conv2d", "lp_conv2d_scratch_bytes", "lp_graph_begin", "lp_graph_end",
     "lp_graph_launch", "lp_conv2d_fwd_noalloc", "LP_NOALLOC_SCRATCH_BYTES", "lp_layer_parallel_step", "lp_auxnet_distill", "lp_aux_correct", "lp_timeline", "lp_timeline_record",
     "LP_PHASE_NAMES", "LP_OP_NAMES", "EXPORTED_SYMBOLS", "lp_selftest_bounded_wait", "lp_call_graphs",
+    "lp_linear_cross_entropy", "lp_linear_cross_entropy_scratch_bytes", "lp_orthogonalize", "lp_orthogonalize_scratch_bytes",
+    "lp_muon_update", "lp_scratch_status",
 ]
 
 LP_OK = 0
@@ -39,7 +41,8 @@ EXPORTED_SYMBOLS = [
     "lp_forward_serial", "lp_serial_fwd_bwd", "lp_get_residual", "lp_last_device_status", "lp_launch_count",
     "lp_conv_profile", "lp_conv2d_scratch_bytes", "lp_conv2d", "lp_graph_begin", "lp_graph_end", "lp_graph_launch",
     "lp_conv2d_fwd_noalloc", "lp_layer_parallel_step", "lp_auxnet_distill", "lp_timeline", "lp_aux_correct",
-    "lp_selftest_bounded_wait", "lp_call_graphs",
+    "lp_selftest_bounded_wait", "lp_call_graphs", "lp_linear_cross_entropy", "lp_linear_cross_entropy_scratch_bytes",
+    "lp_orthogonalize", "lp_orthogonalize_scratch_bytes", "lp_muon_update", "lp_scratch_status",
 ]
 
 
@@ -143,6 +146,14 @@ def library():
     lib.lp_conv2d_scratch_bytes.restype = sz
     lib.lp_conv2d_scratch_bytes.argtypes = [i32, i32, i32]
     lib.lp_conv2d.argtypes = [i32] * 11 + [vp, vp, vp, vp, vp, sz, ctypes.POINTER(f32), vp]
+    lib.lp_linear_cross_entropy_scratch_bytes.restype = sz
+    lib.lp_linear_cross_entropy_scratch_bytes.argtypes = [i32] * 5
+    lib.lp_linear_cross_entropy.argtypes = [i32] * 4 + [vp] * 4 + [f32] + [vp] * 6 + [sz, vp]
+    lib.lp_orthogonalize_scratch_bytes.restype = sz
+    lib.lp_orthogonalize_scratch_bytes.argtypes = [i32] * 4
+    lib.lp_orthogonalize.argtypes = [i32] * 4 + [vp, vp, i32, ctypes.POINTER(f32), f32, vp, sz, vp]
+    lib.lp_muon_update.argtypes = [i32] * 4 + [vp, vp, vp, f32, f32, i32, f32, f32, i32, ctypes.POINTER(f32), f32, vp, sz, vp]
+    lib.lp_scratch_status.argtypes = [vp, vp]
     _LIB = lib
     return lib
 
@@ -423,3 +434,67 @@ def lp_conv2d_fwd_noalloc(N, H, W, Cin, Cout, R, stride, pad, x, w, y, stream=No
     """Forward convolution whose scratch is a fixed array inside the library: for callers that may
     not allocate device memory.  Returns the status (0 = ok); see include/lp.h for the limits."""
     return library().lp_conv2d_fwd_noalloc(N, H, W, Cin, Cout, R, stride, pad, _ptr(x), _ptr(w), _ptr(y), _ptr(stream))
+
+
+def _checked(t, name, dtype, count):
+    """Address of an operand of the stand-alone operators: an address as it is, a tensor if it is one of `count` values of
+    `dtype`, contiguous, on the current device (the operators launch there)."""
+    if t is None or isinstance(t, int):
+        return t
+    import torch
+    if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+        raise ValueError("%s: %d contiguous values of %s are needed, got %s of %s" % (name, count, dtype, tuple(t.shape), t.dtype))
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+    return t.data_ptr()
+
+
+def _operand_dtype(dtype, *tensors):
+    """torch's name of an LP_ dtype; None where no operand is a tensor (addresses need no torch)."""
+    if all(t is None or isinstance(t, int) for t in tensors):
+        return None, None, None
+    import torch
+    return {LP_F32: torch.float32, LP_BF16: torch.bfloat16}.get(dtype), torch.float32, torch.int32
+
+
+def lp_linear_cross_entropy_scratch_bytes(dtype, T, D, V, grads):
+    return library().lp_linear_cross_entropy_scratch_bytes(dtype, T, D, V, 1 if grads else 0)
+
+
+def lp_linear_cross_entropy(dtype, T, D, V, x, w, bias, labels, grad_scale, loss_out, row_loss, dx, dw, dbias, scratch,
+                            scratch_bytes, stream=None):
+    dt, f32, i32 = _operand_dtype(dtype, x, w, bias, labels, loss_out, row_loss, dx, dw, dbias)
+    _check(library().lp_linear_cross_entropy(
+        dtype, T, D, V, _checked(x, "x", dt, T * D), _checked(w, "w", dt, V * D), _checked(bias, "bias", dt, V),
+        _checked(labels, "labels", i32, T), grad_scale, _checked(loss_out, "loss_out", f32, 2),
+        _checked(row_loss, "row_loss", f32, T), _checked(dx, "dx", dt, T * D), _checked(dw, "dw", dt, V * D),
+        _checked(dbias, "dbias", dt, V), _ptr(scratch), scratch_bytes, _ptr(stream)), "lp_linear_cross_entropy")
+
+
+def _coeffs(coeffs):
+    return None if coeffs is None else (ctypes.c_float * 3)(*coeffs)
+
+
+def lp_orthogonalize_scratch_bytes(dtype, batch, rows, cols):
+    return library().lp_orthogonalize_scratch_bytes(dtype, batch, rows, cols)
+
+
+def lp_orthogonalize(dtype, batch, rows, cols, g, out, steps, coeffs, eps, scratch, scratch_bytes, stream=None):
+    dt, _, _ = _operand_dtype(dtype, g, out)
+    n = batch * rows * cols
+    _check(library().lp_orthogonalize(dtype, batch, rows, cols, _checked(g, "g", dt, n), _checked(out, "out", dt, n), steps,
+                                      _coeffs(coeffs), eps, _ptr(scratch), scratch_bytes, _ptr(stream)), "lp_orthogonalize")
+
+
+def lp_muon_update(dtype, batch, rows, cols, w, g, momentum_buf, lr, momentum, nesterov, weight_decay, scale, steps, coeffs,
+                   eps, scratch, scratch_bytes, stream=None):
+    dt, f32, _ = _operand_dtype(dtype, w, g, momentum_buf)
+    n = batch * rows * cols
+    _check(library().lp_muon_update(dtype, batch, rows, cols, _checked(w, "w", dt, n), _checked(g, "g", dt, n),
+                                    _checked(momentum_buf, "momentum_buf", f32, n), lr, momentum, 1 if nesterov else 0,
+                                    weight_decay, scale, steps, _coeffs(coeffs), eps, _ptr(scratch), scratch_bytes,
+                                    _ptr(stream)), "lp_muon_update")
+
+
+def lp_scratch_status(scratch, stream=None):
+    return library().lp_scratch_status(_ptr(scratch), _ptr(stream))

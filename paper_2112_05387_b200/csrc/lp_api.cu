@@ -19,6 +19,7 @@
 #include "conv_tc.cuh"
 #include "conv_tc2.cuh"
 #include "conv_tiles.h"
+#include "device.h"
 #include "kernels_elem.cuh"
 #include "conv_thin.cuh"
 #include "net.h"
@@ -30,9 +31,6 @@ namespace lp {
 // ---------------------------------------------------------------------------------------------
 // small utilities
 // ---------------------------------------------------------------------------------------------
-static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-static inline size_t esize(int dtype) { return dtype == LP_F32 ? 4 : 2; }
-
 enum ExtSlot { EXT_NONE = 0, EXT_X, EXT_XNEXT, EXT_KAPPA, EXT_DX, EXT_IMAGES, EXT_XOUT0 /* + k */ };
 
 struct Tensor {
@@ -202,49 +200,6 @@ struct RunCtx {
   int phase = 0;             // time line: LP_PHASE_*
 };
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-struct Device {
-  bool ready = false;
-  int sm_count = 148;
-  EncodeTiledFn encode = nullptr;
-  // kernel attributes are per device: set on the first launch of each kernel family on that device
-  bool conv_attr = false, wgrad_attr = false, wgrad_halo_attr = false, conv2_attr = false, f32_attr = false, thin_attr = false;
-  int max_pairs = 0;   // CTA pairs of conv_tc2_kernel that can be resident at once (0: not usable)
-  int init() {
-    if (ready) return LP_OK;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return LP_ERR_CUDA;
-    cudaDeviceProp prop;
-    if (cudaGetDeviceProperties(&prop, dev) != cudaSuccess) return LP_ERR_CUDA;
-    sm_count = prop.multiProcessorCount;
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || !fn)
-      return LP_ERR_CUDA;
-    encode = (EncodeTiledFn)fn;
-    if (prop.major != 10) return LP_ERR_UNSUPPORTED;  // the kernels are built for sm_100a only
-    ready = true;
-    return LP_OK;
-  }
-};
-// One record per device ordinal; the current device's record is looked up at every use.  The mutex
-// covers first-use initialisation from several host threads.
-static const int kMaxDevices = 64;
-static Device g_devices[kMaxDevices];
-static std::mutex g_devices_mutex;
-static inline Device& cur_dev() {
-  int d = 0;
-  if (cudaGetDevice(&d) != cudaSuccess || d < 0 || d >= kMaxDevices) d = 0;
-  return g_devices[d];
-}
-static inline int init_cur_dev() {
-  std::lock_guard<std::mutex> lock(g_devices_mutex);
-  return cur_dev().init();
-}
-
 // Per-operation time line: a pair of events around every operation of every plan, on the stream
 // the operation runs on.  Events do not serialise the streams; they cannot be recorded into a graph.
 struct TimelineRec {
@@ -306,20 +261,6 @@ struct lp_handle {
 };
 
 namespace lp {
-
-#define LP_CUDA_OK(expr)                         \
-  do {                                           \
-    cudaError_t e__ = (expr);                    \
-    if (e__ != cudaSuccess) return LP_ERR_CUDA;  \
-  } while (0)
-
-static inline int grid_for(long long work_items, int threads, int sm_count, int per_sm = 8) {
-  long long blocks = (work_items + threads - 1) / threads;
-  long long cap = (long long)sm_count * per_sm;
-  if (blocks > cap) blocks = cap;
-  if (blocks < 1) blocks = 1;
-  return (int)blocks;
-}
 
 // block size that is a multiple of the number of 16-byte channel groups
 static inline int threads_for_channels(int C, int dtype) {
@@ -495,27 +436,6 @@ static int encode_act_map_halo(CUtensorMap* m, const void* base, int N, int H, i
                             CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? LP_OK : LP_ERR_CUDA;
-}
-
-// Launch with a cluster of two CTAs and programmatic stream serialisation allowed.
-template <typename... KArgs, typename... Args>
-static inline cudaError_t launch_pdl_pair(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                                          Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = LP_PDL;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
 // 3x3 stride-1 convolutions with 64-channel K chunks on CTA pairs (conv_tc2.cuh).  Returns LP_ERR_UNSUPPORTED
@@ -2546,7 +2466,6 @@ static size_t boundary_bytes(const lp_handle* h, int k) {   // of x_k
   return (size_t)s.n * s.h * s.w * s.c * esize(h->dtype);
 }
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // `grads_wait`: the gradients are cleared once this event has been reached (the statistics are clear already).  `loss_done`
 // is recorded once the residual exists.

@@ -1,0 +1,392 @@
+// Entry points of the operators at the end of a training step: the loss of a linear layer over many classes
+// (linear_ce.cuh) and the orthogonalised update (ortho.cuh).
+#include <math.h>
+
+#include "../../include/lp.h"
+#include "gemm_launch.h"
+#include "linear_ce.cuh"
+#include "ops.h"
+#include "ortho.cuh"
+
+namespace lp {
+
+// Regions of a scratch buffer, each on a 256-byte boundary.  Without a base it only counts.
+struct Carve {
+  uint8_t* base;
+  size_t off = 0;
+  template <typename T>
+  T* take(size_t n) {
+    T* p = base ? reinterpret_cast<T*>(base + off) : nullptr;
+    off += align_up(n * sizeof(T), 256);
+    return p;
+  }
+};
+static inline long long row_stride(long long cols) { return (cols + 31) / 32 * 32; }   // whole 32-column groups of the epilogues
+
+// ---------------------------------------------------------------------------------------------
+// orthogonalised update
+// ---------------------------------------------------------------------------------------------
+// Powers of two by which the fp16 planes of X, A and B are larger than the matrices: X's entries are about 1 / sqrt(cols),
+// and a low part below 2^-14 would lose bits.  |X| < 16 and |A|, |B| < 63 stay finite.
+static const float kScaleX = 4096.f, kScaleA = 1024.f, kScaleB = 1024.f;
+
+struct OrthoScratch {
+  int* err;
+  float* alpha;
+  double* sums;
+  __half *x[2], *a, *b;
+  int parts;
+  long long ld, ld_s;
+};
+static int ortho_parts(long long elems, int batch) {
+  // blocks of at least 4096 elements, about eight an SM over the batch
+  const long long want = std::max<long long>(1, 1184 / batch), most = std::max<long long>(1, elems / 4096);
+  return (int)std::min<long long>(std::min(want, most), kOrthoMaxParts);
+}
+static OrthoScratch ortho_carve(Carve& c, int batch, int rows, int cols, bool split) {
+  OrthoScratch s;
+  const long long small = std::min(rows, cols);
+  s.ld = row_stride(cols);
+  s.ld_s = row_stride(small);
+  s.parts = ortho_parts((long long)rows * cols, batch);
+  s.err = c.take<int>(64);
+  s.alpha = c.take<float>(batch);
+  s.sums = c.take<double>((size_t)batch * s.parts);
+  const int planes = split ? 2 : 1;
+  for (int i = 0; i < 2; ++i) s.x[i] = c.take<__half>((size_t)2 * batch * rows * s.ld);
+  s.a = c.take<__half>((size_t)planes * batch * small * s.ld_s);
+  s.b = c.take<__half>((size_t)planes * batch * small * s.ld_s);
+  return s;
+}
+size_t ortho_scratch_bytes(int batch, int rows, int cols, bool split) {
+  Carve c{nullptr};
+  ortho_carve(c, batch, rows, cols, split);
+  return c.off;
+}
+
+// Segments of a product of operands kept in `pa` and `pb` planes of `count` matrices each: all products of parts but lo * lo.
+static void gemm_segments(tc::GemmParams& p, int pa, int pb, int count) {
+  p.nseg = 0;
+  for (int i = 0; i < pa; ++i)
+    for (int j = 0; j < pb; ++j) {
+      if (i && j) continue;
+      p.a_z[p.nseg] = i * count;
+      p.b_z[p.nseg] = j * count;
+      ++p.nseg;
+    }
+}
+
+int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* launches) {
+  int rc = gemm_init_dev();
+  if (rc != LP_OK) return rc;
+  const Device& D = cur_dev();
+  Carve c{(uint8_t*)scratch};
+  OrthoScratch s = ortho_carve(c, q.batch, q.rows, q.cols, q.split);
+  const bool tall = q.rows > q.cols;
+  const int small = std::min(q.rows, q.cols), B = q.batch;
+  const long long x_mat = (long long)q.rows * s.ld, x_plane = B * x_mat, s_mat = (long long)small * s.ld_s, s_plane = B * s_mat;
+  const int planes = q.split ? 2 : 1;
+  long long n = 0;
+
+  OrthoSource src;
+  memset(&src, 0, sizeof(src));
+  src.g = q.g; src.g_bf16 = q.g_bf16; src.momentum = q.momentum; src.mu = q.mu; src.nesterov = q.nesterov;
+  src.elems = (long long)q.rows * q.cols;
+  if (q.off) {
+    src.use_off = 1;
+    for (int b = 0; b < B; ++b) src.off[b] = q.off[b];
+  }
+  // bf16 gradients are exact in one plane; a momentum or an fp32 gradient is not
+  int x_planes = (q.g_bf16 && !q.momentum && !q.split) ? 1 : 2;
+  LP_CUDA_OK(launch_pdl(ortho_norm_kernel, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts, s.sums, s.err));
+  LP_CUDA_OK(launch_pdl(ortho_pack_kernel, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts, (const double*)s.sums, q.eps, q.cols,
+                        s.ld, s.x[0], x_mat, x_planes == 2 ? x_plane : 0LL, s.alpha));
+  n += 2;
+
+  // tensor maps, once a call: X in both buffers and both orders, A and B with K contiguous (they are symmetric)
+  CUtensorMap m_xk[2], m_xm[2], m_a, m_b;
+  for (int i = 0; i < 2; ++i) {
+    const GemmOperand x{s.x[i], q.cols, q.rows, s.ld, x_mat, 2 * B, false};
+    if ((rc = encode_gemm_map(&m_xk[i], x, false)) != LP_OK) return rc;
+    if ((rc = encode_gemm_map(&m_xm[i], x, true)) != LP_OK) return rc;
+  }
+  if ((rc = encode_gemm_map(&m_a, GemmOperand{s.a, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
+  if ((rc = encode_gemm_map(&m_b, GemmOperand{s.b, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
+  const bool pair_s = gemm_pair_tiles(small, small, B, true, D.sm_count, D.gemm_pairs);
+  const bool pair_x = gemm_pair_tiles(q.rows, q.cols, B, false, D.sm_count, D.gemm_pairs);
+
+  int cur = 0;
+  for (int i = 0; i < q.steps; ++i) {
+    const bool first = i == 0, last = i + 1 == q.steps;
+    // A = X X^T (X^T X), from the high parts alone unless fp32 results are wanted
+    tc::GemmParams p;
+    memset(&p, 0, sizeof(p));
+    p.M = p.N = small; p.batch = B; p.sym = 1; p.err = s.err;
+    gemm_segments(p, planes, planes, B);
+    p.f = first ? kScaleA : kScaleA / (kScaleX * kScaleX);
+    p.f_dev = s.alpha; p.f_pow = first ? 2 : 0;
+    p.h_out = s.a; p.h_ld = s.ld_s; p.h_batch = s_mat; p.h_plane = q.split ? s_plane : 0;
+    if (tall) rc = launch_gemm<tc::EPI_H16>(p, q.rows, m_xm[cur], true, m_xm[cur], true, false, q.split, pair_s, st);
+    else rc = launch_gemm<tc::EPI_H16>(p, q.cols, m_xk[cur], false, m_xk[cur], false, false, q.split, pair_s, st);
+    if (rc != LP_OK) return rc;
+    // B = a I + b A + c A^2
+    memset(&p, 0, sizeof(p));
+    p.M = p.N = small; p.batch = B; p.sym = 1; p.err = s.err;
+    gemm_segments(p, planes, planes, B);
+    p.f = q.coeffs[2] * (kScaleB / (kScaleA * kScaleA));
+    p.h_out = s.b; p.h_ld = s.ld_s; p.h_batch = s_mat; p.h_plane = q.split ? s_plane : 0;
+    p.aux = s.a; p.aux_f = q.coeffs[1] * (kScaleB / kScaleA); p.diag = q.coeffs[0] * kScaleB;
+    rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, q.split, pair_s, st);
+    if (rc != LP_OK) return rc;
+    // X <- B X (X B).  An error in X grows by up to a in each later step, so its low part is kept while three or more
+    // products follow (relative error of the result, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3 with the
+    // low parts of two steps, 1.1e-3 with all; fp16's step in A and B costs 1e-3)
+    memset(&p, 0, sizeof(p));
+    p.M = q.rows; p.N = q.cols; p.batch = B; p.err = s.err;
+    if (tall) gemm_segments(p, x_planes, planes, B);
+    else gemm_segments(p, planes, x_planes, B);
+    p.f = last ? 1.f / (first ? kScaleB : kScaleB * kScaleX) : (first ? kScaleX / kScaleB : 1.f / kScaleB);
+    p.f_dev = s.alpha; p.f_pow = first ? 1 : 0;
+    const CUtensorMap& ma = tall ? m_xk[cur] : m_b;
+    const CUtensorMap& mb = tall ? m_b : m_xm[cur];
+    if (last) {
+      p.out = q.out; p.out_bf16 = q.out_bf16; p.out_ld = q.cols; p.out_batch = src.elems;
+      p.update = q.update; p.keep = q.keep; p.step = q.step;
+      if (q.off) {
+        p.use_off = 1;
+        for (int b = 0; b < B; ++b) p.off[b] = q.off[b];
+      }
+      rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, q.split, pair_x, st);
+    } else {
+      x_planes = (q.split || i + 3 < q.steps) ? 2 : 1;
+      cur ^= 1;
+      p.h_out = s.x[cur]; p.h_ld = s.ld; p.h_batch = x_mat; p.h_plane = x_planes == 2 ? x_plane : 0;
+      rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, q.split, pair_x, st);
+    }
+    if (rc != LP_OK) return rc;
+    n += 3;
+  }
+  if (launches) *launches += n;
+  return LP_OK;
+}
+
+static const float kOrthoCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
+
+static int check_ortho(int dtype, int batch, int rows, int cols, int steps, float eps) {
+  if (dtype != LP_F32 && dtype != LP_BF16) return LP_ERR_UNSUPPORTED;
+  if (batch < 1 || rows < 1 || cols < 1 || batch > 65535 || steps < 1 || steps > 32) return LP_ERR_SIZE;
+  if ((long long)rows * cols > (1LL << 36) || std::min(rows, cols) > (1 << 17)) return LP_ERR_SIZE;
+  if (!(eps >= 1e-30f) || !(eps <= 1e30f)) return LP_ERR_SIZE;
+  return LP_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// loss of a linear layer
+// ---------------------------------------------------------------------------------------------
+static const size_t kCePieceBytes = (size_t)512 << 20;   // exponentials of a piece of rows
+static const int kCeAmaxParts = 592;
+
+struct CeScratch {
+  CeHeader* hdr;
+  float *amax, *target, *lse, *row_loss, *sums, *acc;
+  float2* stats;
+  __half *p, *x, *w;
+  long long ld_v, ld_d;
+  int rows;                        // of a piece
+  int slab;
+  bool f32, pack_w;
+};
+static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) {
+  CeScratch s;
+  s.f32 = dtype == LP_F32;
+  s.pack_w = s.f32 || D % 8;
+  const int planes = s.f32 ? 2 : 1;
+  s.ld_v = row_stride(V);
+  s.ld_d = (D + 7) / 8 * 8;
+  // (the loss alone keeps 16 bytes for each row and 128 classes)
+  const size_t row_bytes = grads ? (size_t)s.ld_v * 2 * planes : (size_t)((V + 127) / 128) * 16;
+  const long long fit = (long long)(kCePieceBytes / row_bytes) / 256 * 256;
+  s.rows = (int)std::min<long long>(T, std::min(std::max(256LL, fit), 1LL << 18));
+  // rows of a block of the pass over the exponentials: 64, fewer where that leaves SMs idle
+  s.slab = 64;
+  const long long col_blocks = (V + kCeThreads * 8 - 1) / (kCeThreads * 8);
+  while (s.slab > 4 && col_blocks * ((s.rows + s.slab - 1) / s.slab) < 592) s.slab /= 2;
+  s.hdr = c.take<CeHeader>(1);
+  s.amax = c.take<float>(2 * kCeAmaxParts);
+  s.target = c.take<float>(T);
+  s.lse = c.take<float>(T);
+  s.row_loss = c.take<float>(T);
+  s.stats = c.take<float2>((size_t)2 * ((V + 127) / 128) * s.rows);
+  const bool pack_x = s.pack_w || grads;
+  s.x = pack_x ? c.take<__half>((size_t)planes * T * s.ld_d) : nullptr;
+  s.w = s.pack_w ? c.take<__half>((size_t)planes * V * s.ld_d) : nullptr;
+  s.p = grads ? c.take<__half>((size_t)planes * s.rows * s.ld_v) : nullptr;
+  s.sums = grads ? c.take<float>((size_t)((T + s.slab - 1) / s.slab + T / s.rows + 1) * V) : nullptr;
+  s.acc = grads && !s.f32 && s.rows < T ? c.take<float>((size_t)V * D) : nullptr;
+  return s;
+}
+
+}  // namespace lp
+
+using namespace lp;
+
+extern "C" {
+
+size_t lp_orthogonalize_scratch_bytes(int dtype, int batch, int rows, int cols) {
+  if (check_ortho(dtype, batch, rows, cols, 1, 1.f) != LP_OK) return 0;
+  return ortho_scratch_bytes(batch, rows, cols, dtype == LP_F32);
+}
+
+int lp_orthogonalize(int dtype, int batch, int rows, int cols, const void* g, void* out, int steps, const float* coeffs, float eps,
+                     void* scratch, size_t scratch_bytes, void* stream) {
+  if (!g || !out || !scratch) return LP_ERR_NULL;
+  int rc = check_ortho(dtype, batch, rows, cols, steps, eps);
+  if (rc != LP_OK) return rc;
+  if (!aligned16(g) || !aligned16(out) || (reinterpret_cast<uintptr_t>(scratch) & 255)) return LP_ERR_ALIGN;
+  if (scratch_bytes < lp_orthogonalize_scratch_bytes(dtype, batch, rows, cols)) return LP_ERR_WORKSPACE;
+  OrthoProblem q;
+  memset(&q, 0, sizeof(q));
+  q.batch = batch; q.rows = rows; q.cols = cols;
+  q.g_bf16 = q.out_bf16 = dtype == LP_BF16;
+  q.split = dtype == LP_F32;
+  q.g = g; q.out = out; q.steps = steps; q.eps = eps;
+  memcpy(q.coeffs, coeffs ? coeffs : kOrthoCoeffs, sizeof(q.coeffs));
+  return ortho_run(q, scratch, (cudaStream_t)stream, nullptr);
+}
+
+int lp_muon_update(int dtype, int batch, int rows, int cols, void* w, const void* g, float* momentum_buf, float lr, float momentum,
+                   int nesterov, float weight_decay, float scale, int steps, const float* coeffs, float eps, void* scratch,
+                   size_t scratch_bytes, void* stream) {
+  if (!w || !g || !momentum_buf || !scratch) return LP_ERR_NULL;
+  int rc = check_ortho(dtype, batch, rows, cols, steps, eps);
+  if (rc != LP_OK) return rc;
+  if (!aligned16(w) || !aligned16(g) || !aligned16(momentum_buf) || (reinterpret_cast<uintptr_t>(scratch) & 255)) return LP_ERR_ALIGN;
+  if (scratch_bytes < lp_orthogonalize_scratch_bytes(dtype, batch, rows, cols)) return LP_ERR_WORKSPACE;
+  OrthoProblem q;
+  memset(&q, 0, sizeof(q));
+  q.batch = batch; q.rows = rows; q.cols = cols;
+  q.g_bf16 = q.out_bf16 = dtype == LP_BF16;
+  q.split = dtype == LP_F32;
+  q.g = g; q.momentum = momentum_buf; q.mu = momentum; q.nesterov = nesterov != 0;
+  q.out = w; q.update = true; q.keep = 1.f - lr * weight_decay; q.step = -lr * scale;
+  q.steps = steps; q.eps = eps;
+  memcpy(q.coeffs, coeffs ? coeffs : kOrthoCoeffs, sizeof(q.coeffs));
+  return ortho_run(q, scratch, (cudaStream_t)stream, nullptr);
+}
+
+size_t lp_linear_cross_entropy_scratch_bytes(int dtype, int T, int D, int V, int grads) {
+  if ((dtype != LP_F32 && dtype != LP_BF16) || T < 1 || D < 1 || V < 1) return 0;
+  Carve c{nullptr};
+  ce_carve(c, dtype, T, D, V, grads != 0);
+  return c.off;
+}
+
+int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const void* w, const void* bias, const int32_t* labels,
+                            float grad_scale, float* loss_out, float* row_loss, void* dx, void* dw, void* dbias, void* scratch,
+                            size_t scratch_bytes, void* stream) {
+  if (!x || !w || !labels || !loss_out || !scratch) return LP_ERR_NULL;
+  if (dtype != LP_F32 && dtype != LP_BF16) return LP_ERR_UNSUPPORTED;
+  if (T < 1 || D < 1 || V < 1) return LP_ERR_SIZE;
+  const void* ptrs[] = {x, w, bias, labels, loss_out, row_loss, dx, dw, dbias};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return LP_ERR_ALIGN;
+  if (reinterpret_cast<uintptr_t>(scratch) & 255) return LP_ERR_ALIGN;
+  const bool grads = dx || dw || dbias;
+  if (scratch_bytes < lp_linear_cross_entropy_scratch_bytes(dtype, T, D, V, grads)) return LP_ERR_WORKSPACE;
+  int rc = gemm_init_dev();
+  if (rc != LP_OK) return rc;
+  const Device& Dv = cur_dev();
+  cudaStream_t st = (cudaStream_t)stream;
+  Carve c{(uint8_t*)scratch};
+  const CeScratch s = ce_carve(c, dtype, T, D, V, grads);
+  const int planes = s.f32 ? 2 : 1, is_bf16 = !s.f32;
+  const long long x_plane = (long long)T * s.ld_d, w_plane = (long long)V * s.ld_d, p_plane = (long long)s.rows * s.ld_v;
+  float* rl = row_loss ? row_loss : s.row_loss;
+  const int amax_blocks = s.f32 ? 2 * kCeAmaxParts : 0;
+  LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + amax_blocks), dim3(kCeThreads), 0, st, labels, T, V, (const float*)x, (long long)T * D,
+                        (const float*)w, (long long)V * D, s.amax, kCeAmaxParts, s.hdr));
+  if (s.x) {
+    const int xb = grid_for((long long)T * D, kCeThreads * 8, Dv.sm_count, 4);
+    const int wb = s.w ? grid_for((long long)V * D, kCeThreads * 8, Dv.sm_count, 8) : 0;
+    LP_CUDA_OK(launch_pdl(ce_pack_kernel, dim3(xb + wb), dim3(kCeThreads), 0, st, x, w, labels, is_bf16, T, D, V, s.ld_d, s.x, x_plane, s.w,
+                          w_plane, xb, (const float*)s.amax, kCeAmaxParts, grad_scale, s.hdr));
+  }
+  const void* xm = s.x ? (const void*)s.x : x;
+  const void* wm = s.w ? (const void*)s.w : w;
+  const long long ldx = s.x ? s.ld_d : D, ldw = s.w ? s.ld_d : D;
+  CUtensorMap m_wk, m_wm;
+  const GemmOperand ow{wm, D, V, ldw, w_plane, planes, !s.f32};
+  if ((rc = encode_gemm_map(&m_wk, ow, false)) != LP_OK) return rc;
+  if ((rc = encode_gemm_map(&m_wm, ow, true)) != LP_OK) return rc;
+  int slab0 = 0;
+  for (int r0 = 0; r0 < T; r0 += s.rows) {
+    const int rows = std::min(s.rows, T - r0);
+    const GemmOperand ox{(const uint16_t*)xm + (long long)r0 * ldx, D, rows, ldx, x_plane, planes, !s.f32};
+    CUtensorMap m_xk, m_xm, m_pk, m_pm;
+    if ((rc = encode_gemm_map(&m_xk, ox, false)) != LP_OK) return rc;
+    const bool pair = gemm_pair_tiles(rows, V, 1, false, Dv.sm_count, Dv.gemm_pairs);
+    const int part_cols = pair ? 128 : 64, parts = (V + (pair ? 255 : 127)) / (pair ? 256 : 128) * 2;
+    tc::GemmParams p;
+    memset(&p, 0, sizeof(p));
+    p.M = rows; p.N = V; p.batch = 1; p.err = &s.hdr->err;
+    gemm_segments(p, planes, planes, 1);
+    p.f = 1.f; p.f_dev = &s.hdr->logit_f; p.f_pow = s.f32 ? 1 : 0;
+    p.bias = bias; p.bias_bf16 = is_bf16; p.labels = labels + r0;
+    p.stats = s.stats; p.stats_ld = s.rows; p.target = s.target + r0;
+    p.h_out = s.p; p.h_ld = s.ld_v; p.h_plane = s.f32 ? p_plane : 0;
+    if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, s.f32, pair, st)) != LP_OK) return rc;
+    LP_CUDA_OK(launch_pdl(ce_rows_kernel, dim3((rows + 31) / 32), dim3(kCeThreads), 0, st, (const float2*)s.stats, (long long)s.rows, parts,
+                          rows, V, labels + r0, (const float*)(s.target + r0), s.lse + r0, rl + r0));
+    if (!grads) continue;
+    const int slabs = (rows + s.slab - 1) / s.slab;
+    const dim3 gd((V + kCeThreads * 8 - 1) / (kCeThreads * 8), slabs);
+    float* sums = dbias ? s.sums + (long long)slab0 * V : nullptr;
+    LP_CUDA_OK(launch_pdl(s.f32 ? ce_dl_kernel<true> : ce_dl_kernel<false>, gd, dim3(kCeThreads), 0, st, s.p, s.ld_v, p_plane, rows, V, s.slab,
+                          (const float2*)s.stats, (long long)s.rows, part_cols, (const float*)(s.lse + r0), (const float*)(s.target + r0),
+                          labels + r0, sums));
+    slab0 += slabs;
+    const GemmOperand op{s.p, V, rows, s.ld_v, p_plane, planes, !s.f32};
+    if (dx) {
+      if ((rc = encode_gemm_map(&m_pk, op, false)) != LP_OK) return rc;
+      memset(&p, 0, sizeof(p));
+      p.M = rows; p.N = D; p.batch = 1; p.err = &s.hdr->err;
+      gemm_segments(p, planes, planes, 1);
+      p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1;
+      p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
+      const bool pr = gemm_pair_tiles(rows, D, 1, false, Dv.sm_count, Dv.gemm_pairs);
+      if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, s.f32, pr, st)) != LP_OK) return rc;
+    }
+    if (dw) {
+      if ((rc = encode_gemm_map(&m_pm, op, true)) != LP_OK) return rc;
+      if ((rc = encode_gemm_map(&m_xm, ox, true)) != LP_OK) return rc;
+      memset(&p, 0, sizeof(p));
+      p.M = V; p.N = D; p.batch = 1; p.err = &s.hdr->err;
+      gemm_segments(p, planes, planes, 1);
+      p.f = 1.f; p.f_dev = &s.hdr->dw_f; p.f_pow = 1;
+      p.out = dw; p.out_bf16 = is_bf16; p.out_ld = D;
+      if (s.rows < T) {
+        p.acc = s.f32 ? (float*)dw : s.acc;
+        p.acc_first = r0 == 0;
+        p.acc_last = r0 + rows == T;
+      }
+      const bool pr = gemm_pair_tiles(V, D, 1, false, Dv.sm_count, Dv.gemm_pairs);
+      if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, s.f32, pr, st)) != LP_OK) return rc;
+    }
+  }
+  if (dbias)
+    LP_CUDA_OK(launch_pdl(ce_dbias_kernel, dim3((V + kCeThreads - 1) / kCeThreads), dim3(kCeThreads), 0, st, (const float*)s.sums, slab0, V,
+                          (const CeHeader*)s.hdr, dbias, is_bf16));
+  LP_CUDA_OK(launch_pdl(ce_loss_kernel, dim3(1), dim3(kCeThreads), 0, st, (const float*)rl, T, (const CeHeader*)s.hdr, loss_out));
+  return LP_OK;
+}
+
+int lp_scratch_status(const void* scratch, void* stream) {
+  if (!scratch) return LP_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(scratch) & 255) return LP_ERR_ALIGN;
+  LP_CUDA_OK(cudaStreamSynchronize((cudaStream_t)stream));
+  int e = 0;
+  LP_CUDA_OK(cudaMemcpy(&e, scratch, sizeof(e), cudaMemcpyDeviceToHost));
+  return e ? LP_ERR_DEVICE_TIMEOUT : LP_OK;
+}
+
+}  // extern "C"

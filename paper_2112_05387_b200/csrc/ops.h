@@ -1,0 +1,30 @@
+// The orthogonalised update as lp_step_muon and the stand-alone entry points run it.
+#pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
+
+namespace lp {
+
+struct OrthoProblem {
+  int batch, rows, cols;
+  bool g_bf16;            // type of g
+  bool split;             // fp32 results: operands as high and low parts
+  const void* g;
+  const long long* off;   // element offset of each matrix from g, momentum and out (host, `batch` of them), or null: contiguous
+  float* momentum;        // or null
+  float mu;
+  bool nesterov;
+  int steps;
+  float coeffs[3];
+  float eps;
+  void* out;              // result, or the weights that are updated
+  bool out_bf16;
+  bool update;            // out <- keep * out + step * O
+  float keep, step;
+};
+
+size_t ortho_scratch_bytes(int batch, int rows, int cols, bool split);
+// Enqueues the operator; `launches` (nullable) counts its kernels.
+int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* launches);
+
+}  // namespace lp
