@@ -30,12 +30,10 @@ static int encode_gemm_map(CUtensorMap* m, const GemmOperand& o, bool mn) {
   return r == CUDA_SUCCESS ? LP_OK : LP_ERR_CUDA;
 }
 
-template <int kEpi>
-static int gemm_set_attributes(Device& D) {
-  LP_CUDA_OK(cudaFuncSetAttribute(tc::gemm_tc_kernel<kEpi, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc::kGemmSmem));
-  LP_CUDA_OK(cudaFuncSetAttribute(tc::gemm_tc_kernel<kEpi, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc::kGemmSmem));
-  LP_CUDA_OK(cudaFuncSetAttribute(tc::gemm_tc_kernel<kEpi, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc::kGemmSmem));
-  LP_CUDA_OK(cudaFuncSetAttribute(tc::gemm_tc_kernel<kEpi, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc::kGemmSmem));
+template <int kEpi, int kMode>
+static int gemm_set_attributes() {
+  LP_CUDA_OK(cudaFuncSetAttribute(tc::gemm_tc_kernel<kEpi, true, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc::kGemmSmem));
+  LP_CUDA_OK(cudaFuncSetAttribute(tc::gemm_tc_kernel<kEpi, false, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc::kGemmSmem));
   return LP_OK;
 }
 // Kernel attributes, and how many CTA pairs the device holds at once (the grid is persistent: never more than that).
@@ -45,9 +43,12 @@ static int gemm_init_dev() {
   std::lock_guard<std::mutex> lock(g_devices_mutex);
   Device& D = cur_dev();
   if (D.gemm_attr) return LP_OK;
-  if ((rc = gemm_set_attributes<tc::EPI_H16>(D)) != LP_OK) return rc;
-  if ((rc = gemm_set_attributes<tc::EPI_OUT>(D)) != LP_OK) return rc;
-  if ((rc = gemm_set_attributes<tc::EPI_CE>(D)) != LP_OK) return rc;
+  using namespace tc;
+  if ((rc = gemm_set_attributes<EPI_H16, GEMM_ONE>()) != LP_OK || (rc = gemm_set_attributes<EPI_H16, GEMM_LOW>()) != LP_OK ||
+      (rc = gemm_set_attributes<EPI_H16, GEMM_SPLIT>()) != LP_OK || (rc = gemm_set_attributes<EPI_OUT, GEMM_ONE>()) != LP_OK ||
+      (rc = gemm_set_attributes<EPI_OUT, GEMM_LOW>()) != LP_OK || (rc = gemm_set_attributes<EPI_OUT, GEMM_SPLIT>()) != LP_OK ||
+      (rc = gemm_set_attributes<EPI_CE, GEMM_ONE>()) != LP_OK || (rc = gemm_set_attributes<EPI_CE, GEMM_SPLIT>()) != LP_OK)
+    return rc;
   cudaLaunchConfig_t q = {};
   q.gridDim = dim3(2 * D.sm_count);
   q.blockDim = dim3(tc::kGemmThreads);
@@ -58,7 +59,7 @@ static int gemm_init_dev() {
   q.attrs = qa;
   q.numAttrs = 1;
   int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, tc::gemm_tc_kernel<tc::EPI_OUT, true, false>, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
+  if (cudaOccupancyMaxActiveClusters(&n, tc::gemm_tc_kernel<tc::EPI_OUT, true, tc::GEMM_ONE>, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
   D.gemm_pairs = n;
   D.gemm_attr = true;
   return LP_OK;
@@ -76,15 +77,24 @@ static bool gemm_pair_tiles(long long M, long long N, int batch, bool sym, int s
   return pair <= single;
 }
 
-// K steps (of 64 wide blocks and segments) that the tensor core adds up before its accumulator is emptied into registers
-// where fp32 results are wanted.
-constexpr int kGemmRound = 12;
+// K blocks of 64 that the tensor core adds up before its accumulator is emptied into registers where fp32 results are wanted.
+#ifndef LP_GEMM_ROUND
+#define LP_GEMM_ROUND 1
+#endif
+constexpr int kGemmRound = LP_GEMM_ROUND;
 
-// Launches the product.  Sizes, segments and the epilogue's fields of `p` are the caller's; the rest is filled in here.
+template <int kEpi, int kMode>
+static cudaError_t start_gemm(const tc::GemmParams& p, const CUtensorMap& ma, const CUtensorMap& mb, bool pair, cudaStream_t st) {
+  const Device& D = cur_dev();
+  const dim3 block(tc::kGemmThreads);
+  return pair ? launch_pdl_pair(tc::gemm_tc_kernel<kEpi, true, kMode>, dim3(2 * std::min(p.total_tiles, D.gemm_pairs)), block, tc::kGemmSmem, st,
+                                ma, mb, p)
+              : launch_pdl(tc::gemm_tc_kernel<kEpi, false, kMode>, dim3(std::min(p.total_tiles, D.sm_count)), block, tc::kGemmSmem, st, ma, mb, p);
+}
+// Launches the product.  Sizes, planes and the epilogue's fields of `p` are the caller's; the rest is filled in here.
 template <int kEpi>
 static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bool a_mn, const CUtensorMap& mb, bool b_mn, bool bf16,
-                       bool rounds, bool pair, cudaStream_t st) {
-  const Device& D = cur_dev();
+                       bool pair, cudaStream_t st) {
   const int tile = pair ? 256 : 128;
   p.tiles_m = (p.M + tile - 1) / tile;
   p.tiles_n = (p.N + tile - 1) / tile;
@@ -98,17 +108,18 @@ static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bo
   p.b_mn = b_mn;
   // operand format: bits 7 and 10 (bf16) on top of fp32 accumulation and the shape
   p.idesc = tc::instr_desc_bf16(tile, tile, a_mn, b_mn) & ~(bf16 ? 0u : ((1u << 7) | (1u << 10)));
-  const dim3 block(tc::kGemmThreads);
-  cudaError_t e;
-  if (pair) {
-    const dim3 grid(2 * std::min(p.total_tiles, D.gemm_pairs));
-    e = rounds ? launch_pdl_pair(tc::gemm_tc_kernel<kEpi, true, true>, grid, block, tc::kGemmSmem, st, ma, mb, p)
-               : launch_pdl_pair(tc::gemm_tc_kernel<kEpi, true, false>, grid, block, tc::kGemmSmem, st, ma, mb, p);
-  } else {
-    const dim3 grid(std::min(p.total_tiles, D.sm_count));
-    e = rounds ? launch_pdl(tc::gemm_tc_kernel<kEpi, false, true>, grid, block, tc::kGemmSmem, st, ma, mb, p)
-               : launch_pdl(tc::gemm_tc_kernel<kEpi, false, false>, grid, block, tc::kGemmSmem, st, ma, mb, p);
+  if (kEpi == tc::EPI_OUT) {
+    const long long unit = p.out_bf16 ? 16 : 8;
+    bool vec = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0 && p.out_ld % unit == 0 && p.N % unit == 0 && p.out_batch % unit == 0;
+    if (p.acc) vec = vec && (reinterpret_cast<uintptr_t>(p.acc) & 31) == 0 && p.N % 8 == 0;
+    for (int b = 0; p.use_off && b < p.batch; ++b) vec = vec && p.off[b] % unit == 0;
+    p.out_vec = vec;
   }
+  cudaError_t e;
+  if (p.a_planes == 1 && p.b_planes == 1) e = start_gemm<kEpi, tc::GEMM_ONE>(p, ma, mb, pair, st);
+  else if (p.a_planes == 2 && p.b_planes == 2) e = start_gemm<kEpi, tc::GEMM_SPLIT>(p, ma, mb, pair, st);
+  else if constexpr (kEpi != tc::EPI_CE) e = start_gemm<kEpi, tc::GEMM_LOW>(p, ma, mb, pair, st);
+  else return LP_ERR_UNSUPPORTED;
   LP_CUDA_OK(e);
   return LP_OK;
 }

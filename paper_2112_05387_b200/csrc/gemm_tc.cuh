@@ -8,10 +8,11 @@
 // The grid is persistent: a CTA (pair) walks the tiles, six stages of operands in flight, two accumulators in tensor
 // memory, so that a tile's epilogue runs under the next tile's products.
 //
-// Precision.  A product may be a sum of several: operands kept as a 16-bit high and a low part (planes of the same
-// tensor) are multiplied as hi*hi + hi*lo + lo*hi in one accumulation (`nseg`, planes per segment).  Where fp32 results are
-// wanted (kRounds), the tensor core's accumulator is emptied every `round_len` K blocks into registers and added up there:
-// the accumulation inside the tensor core does not round to nearest, and its error grows with the number of K steps.
+// Precision.  Operands may be kept as a 16-bit high and a low part (planes of the same tensor): a stage holds all planes of
+// its K block, and hi*hi + hi*lo + lo*hi go into one accumulation (four tiles fetched for three products; lo*lo is below what
+// the parts keep).  Where fp32 results are wanted (kRounds), the tensor core's accumulator is emptied every `round_len` K
+// blocks into registers and added up there: the accumulation inside the tensor core does not round to nearest, and its error
+// grows with the number of K steps.
 //
 // Roles (320 threads): warp 0 TMA producer, warp 1 MMA issuer (of the pair's leader), warps 2..9 epilogue: two warps per
 // quarter of the accumulator's rows, each taking one half of its columns; a thread has one row.
@@ -24,11 +25,12 @@
 namespace lp {
 namespace tc {
 
-constexpr int kGemmStages = 6;
+constexpr int kGemmStages = 6;                 // at most: 6 of one plane of each operand, 4 of three planes, 3 of four
 constexpr int kGemmThreads = 320;
 constexpr int kGemmEpiWarps = 8;
-constexpr uint32_t kGemmStageBytes = 32768;   // 128 rows x 64 columns of A and of B, 16 bits each
-constexpr int kGemmScratchFloats = 32 * 33;   // per epilogue warp: a 32 x 32 block, to be written row by row
+constexpr uint32_t kGemmTileBytes = 16384;    // 128 rows x 64 columns of a plane, 16 bits each
+constexpr uint32_t kGemmRingBytes = 12 * kGemmTileBytes;
+constexpr int kGemmScratchFloats = 32 * 33;   // per epilogue warp: a 32 x 32 block, written row by row where rows are not aligned
 constexpr int kGemmMaxOffsets = 64;
 
 struct GemmTail {
@@ -37,7 +39,7 @@ struct GemmTail {
   uint32_t tmem_base;
   int abort_flag;
 };
-constexpr size_t kGemmSmem = 1024 + (size_t)kGemmStages * kGemmStageBytes + (size_t)kGemmEpiWarps * kGemmScratchFloats * 4 + sizeof(GemmTail);
+constexpr size_t kGemmSmem = 1024 + (size_t)kGemmRingBytes + (size_t)kGemmEpiWarps * kGemmScratchFloats * 4 + sizeof(GemmTail);
 static_assert(kGemmSmem <= 232448, "shared memory of a block");
 
 enum GemmEpi {
@@ -51,9 +53,9 @@ struct GemmParams {
   int tiles_m, tiles_n, total_tiles;
   int sym;                        // D is symmetric: tiles on and above the diagonal, written to both places (M = N)
   int group_m;                    // row tiles that are walked together (they share B tiles in L2)
-  int kblocks, nseg;
-  int a_z[3], b_z[3];             // first plane of each segment's operands
-  int round_len;                  // kRounds: (K block, segment) steps per accumulation
+  int kblocks;
+  int a_planes, b_planes;         // parts of each operand (1 or 2), `batch` matrices apart
+  int round_len;                  // kRounds: K blocks per accumulation
   int a_mn, b_mn;                 // 1: the operand's row index is the contiguous one
   uint32_t idesc;
   int* err;
@@ -68,7 +70,7 @@ struct GemmParams {
   float aux_f, diag;
   // EPI_OUT
   void* out;
-  int out_bf16;
+  int out_bf16, out_vec;          // out_vec: every row of out (and acc) starts on 32 bytes and N is a multiple of 32 bytes
   long long out_ld, out_batch;
   float* acc;                     // fp32 sums over pieces, [M][N], or null
   int acc_first, acc_last;        // first piece: stored, not added; last piece: the result goes to `out`
@@ -132,95 +134,170 @@ __device__ __forceinline__ void half2_floats(uint32_t u, float& a, float& b) {
   b = f.y;
 }
 
-// One 32-column group of EPI_H16.  `row` < M; columns from `col` on; the group may run past N (the buffer's rows are
-// padded to whole groups of 32 columns, and what lies there is never read).
-__device__ __forceinline__ void epi_h16(const GemmParams& p, int b, int row, int col, bool mirror, float f, const float (&v)[32]) {
-  if (col >= p.N) return;
-  const bool valid = row < p.M;
-  __half* dst = p.h_out + b * p.h_batch + (long long)row * p.h_ld + col;
-  float w[32];
-#pragma unroll
-  for (int j = 0; j < 32; ++j) w[j] = f * v[j];
-  if (p.aux && valid) {
-    const __half* a = p.aux + b * p.h_batch + (long long)row * p.h_ld + col;
+// 32-byte global accesses (addresses are 32-byte aligned): a thread has a row of the accumulator, and what it reads or writes of
+// 32 columns there goes by whole sectors.  Not through shared memory: at 64 bytes a cycle written by the loads and 64 read by
+// the products, the rings leave none of its bandwidth (a pass through scratch cost the mainloop 10 % at K = 2048).
+__device__ __forceinline__ void st_v8(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ void st_v8f(float* p, const float* v) {
+  const uint32_t u[8] = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]),
+                         __float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+  st_v8(p, u);
+}
+__device__ __forceinline__ void ld_v8(const void* p, uint32_t* v) {
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "l"(p)
+               : "memory");
+}
+
+// One 32-column group of an intermediate, as fp16 planes.  Columns past N are written as far as the buffer's rows are padded
+// (whole groups of 32); what lies there is never read.  `mirror`: the block above the diagonal of a symmetric result goes below
+// it, too.
+__device__ __forceinline__ void epi_h16(const GemmParams& p, int b, int row, int col, bool mirror, float (&v)[32]) {
+  if (row >= p.M) return;
+  const long long at = b * p.h_batch + (long long)row * p.h_ld + col;
+  if (p.aux) {
 #pragma unroll
     for (int pl = 0; pl < 2; ++pl) {
       if (pl && !p.h_plane) break;
+      uint32_t x[16];
+      ld_v8(p.aux + pl * p.h_plane + at, x);
+      ld_v8(p.aux + pl * p.h_plane + at + 16, x + 8);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint4 q = *reinterpret_cast<const uint4*>(a + pl * p.h_plane + 8 * u);
-        const uint32_t x[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float lo, hi;
-          half2_floats(x[i], lo, hi);
-          w[8 * u + 2 * i] = fmaf(p.aux_f, lo, w[8 * u + 2 * i]);
-          w[8 * u + 2 * i + 1] = fmaf(p.aux_f, hi, w[8 * u + 2 * i + 1]);
-        }
+      for (int i = 0; i < 16; ++i) {
+        float lo, hi;
+        half2_floats(x[i], lo, hi);
+        v[2 * i] = fmaf(p.aux_f, lo, v[2 * i]);
+        v[2 * i + 1] = fmaf(p.aux_f, hi, v[2 * i + 1]);
       }
     }
 #pragma unroll
     for (int j = 0; j < 32; ++j)
-      if (col + j == row) w[j] += p.diag;
+      if (col + j == row) v[j] += p.diag;
   }
-  __half hi[32], lo[32];
-#pragma unroll
-  for (int j = 0; j < 32; ++j) split_half(w[j], hi[j], lo[j]);
 #pragma unroll
   for (int pl = 0; pl < 2; ++pl) {
     if (pl && !p.h_plane) break;
-    const __half(&h)[32] = pl ? lo : hi;
-    if (valid) {
+    __half* out = p.h_out + pl * p.h_plane + b * p.h_batch;
+    uint32_t h[16];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        *reinterpret_cast<uint4*>(dst + pl * p.h_plane + 8 * u) =
-            make_uint4(pack_half2(h[8 * u], h[8 * u + 1]), pack_half2(h[8 * u + 2], h[8 * u + 3]),
-                       pack_half2(h[8 * u + 4], h[8 * u + 5]), pack_half2(h[8 * u + 6], h[8 * u + 7]));
-      if (mirror) {   // the lanes hold consecutive rows: 64 bytes of row `col + j` of the mirrored tile
-        __half* m = p.h_out + pl * p.h_plane + b * p.h_batch + (long long)col * p.h_ld + row;
+    for (int i = 0; i < 16; ++i) {
+      const __half h0 = __float2half_rn(v[2 * i]), h1 = __float2half_rn(v[2 * i + 1]);
+      h[i] = pack_half2(h0, h1);
+      v[2 * i] -= __half2float(h0);       // what the low part holds
+      v[2 * i + 1] -= __half2float(h1);
+    }
+    st_v8(out + (long long)row * p.h_ld + col, h);
+    st_v8(out + (long long)row * p.h_ld + col + 16, h + 8);
+    if (mirror) {   // the lanes hold consecutive rows: 64 bytes of row `col + j` of the mirrored block
+      __half* m = out + (long long)col * p.h_ld + row;
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (col + j < p.N) m[(long long)j * p.h_ld] = h[j];
-      }
+      for (int j = 0; j < 32; ++j)
+        if (col + j < p.N) m[j * p.h_ld] = __ushort_as_half((unsigned short)(j & 1 ? h[j >> 1] >> 16 : h[j >> 1] & 0xFFFFu));
     }
   }
 }
 
-// One 32-column group of EPI_OUT: through the warp's scratch, so that a row's 32 values leave in one access whatever the
-// row stride of the result (any M, N, alignment of the element type).
-__device__ __forceinline__ void epi_out(const GemmParams& p, int b, int row0, int col, float f, const float (&v)[32], float* scratch,
-                                        int lane) {
-  if (col >= p.N) return;
+// One 32-column group of a result in the caller's type whose rows are 32-byte aligned (and N a multiple of 32 bytes of it).
+// What is added to, or updated, is read before anything is written: its reads are in flight together.
+__device__ __forceinline__ void epi_out_vec(const GemmParams& p, int b, int row, int col, float (&v)[32]) {
+  if (row >= p.M) return;
+  const int n = min(32, p.N - col);
+  if (p.acc) {
+    float* acc = p.acc + (long long)row * p.N + col;
+    if (!p.acc_first) {
+      uint32_t x[32];
 #pragma unroll
-  for (int j = 0; j < 32; ++j) scratch[lane * 33 + j] = f * v[j];
-  __syncwarp();
-  const int rows = min(32, p.M - row0);
-  const bool ok = col + lane < p.N;
-  const long long at = (p.use_off ? p.off[b] : b * p.out_batch) + (long long)row0 * p.out_ld + col + lane;
-  const long long acc_at = (long long)row0 * p.N + col + lane;
-#pragma unroll 8
-  for (int r = 0; r < rows; ++r) {
-    if (ok) {
-      float x = scratch[r * 33 + lane];
-      if (p.acc) {
-        float* s = p.acc + acc_at + (long long)r * p.N;
-        if (!p.acc_first) x += *s;
-        if (!p.acc_last) *s = x;
-      }
-      if (!p.acc || p.acc_last) {
-        if (p.out_bf16) {
-          bf16* o = (bf16*)p.out + at + (long long)r * p.out_ld;
-          if (p.update) x = fmaf(p.step, x, p.keep * __bfloat162float(*o));
-          *o = __float2bfloat16_rn(x);
-        } else {
-          float* o = (float*)p.out + at + (long long)r * p.out_ld;
-          if (p.update) x = fmaf(p.step, x, p.keep * *o);
-          *o = x;
-        }
-      }
+      for (int u = 0; u < 4; ++u)
+        if (8 * u < n) ld_v8(acc + 8 * u, x + 8 * u);
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (j < n) v[j] += __uint_as_float(x[j]);
+    }
+    if (!p.acc_last) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (8 * u < n) st_v8f(acc + 8 * u, v + 8 * u);
+      return;
     }
   }
+  const long long at = (p.use_off ? p.off[b] : b * p.out_batch) + (long long)row * p.out_ld + col;
+  if (p.out_bf16) {
+    bf16* o = (bf16*)p.out + at;
+    uint32_t x[16];
+    if (p.update) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (16 * u < n) ld_v8(o + 16 * u, x + 8 * u);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        v[2 * i] = fmaf(p.step, v[2 * i], p.keep * __uint_as_float(x[i] << 16));
+        v[2 * i + 1] = fmaf(p.step, v[2 * i + 1], p.keep * __uint_as_float(x[i] & 0xFFFF0000u));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (16 * u < n) st_v8(o + 16 * u, x + 8 * u);
+  } else {
+    float* o = (float*)p.out + at;
+    if (p.update) {
+      uint32_t x[32];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (8 * u < n) ld_v8(o + 8 * u, x + 8 * u);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = fmaf(p.step, v[j], p.keep * __uint_as_float(x[j]));
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (8 * u < n) st_v8f(o + 8 * u, v + 8 * u);
+  }
+}
+
+// The same for any row stride: through the warp's scratch, so that a row's 32 values leave in one access.  Eight rows at a
+// time: their reads are in flight together.
+template <typename T>
+__device__ __forceinline__ void rows_to(T* out, long long ld, int rows, float* scratch, bool add, float keep, float step) {
+#pragma unroll 1
+  for (int r = 0; r < rows; r += 8) {
+    if (add) {
+      T old[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r + i < rows) old[i] = out[(r + i) * ld];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r + i < rows) from_f(out[(r + i) * ld], fmaf(step, scratch[(r + i) * 33], keep * to_f(old[i])));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r + i < rows) from_f(out[(r + i) * ld], scratch[(r + i) * 33]);
+    }
+  }
+}
+__device__ __forceinline__ void epi_out_any(const GemmParams& p, int b, int row0, int col, const float (&v)[32], float* scratch, int lane) {
   __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 32; ++j) scratch[lane * 33 + j] = v[j];
+  __syncwarp();
+  if (col + lane >= p.N) return;
+  const int rows = min(32, p.M - row0);
+  scratch += lane;
+  if (p.acc) {
+    float* acc = p.acc + (long long)row0 * p.N + col + lane;
+    rows_to(acc, p.N, rows, scratch, !p.acc_first, 1.f, 1.f);
+    if (!p.acc_last) return;
+    for (int r = 0; r < rows; ++r) scratch[r * 33] = acc[(long long)r * p.N];   // (this lane's own sums)
+  }
+  const long long at = (p.use_off ? p.off[b] : b * p.out_batch) + (long long)row0 * p.out_ld + col + lane;
+  if (p.out_bf16) rows_to((bf16*)p.out + at, p.out_ld, rows, scratch, p.update, p.keep, p.step);
+  else rows_to((float*)p.out + at, p.out_ld, rows, scratch, p.update, p.keep, p.step);
 }
 
 // Logits of a 32-column group: scale, bias, and -inf past the last class.
@@ -244,13 +321,20 @@ constexpr float kLog2e = 1.4426950408889634f;
 // Exponentials are kept 2^14 times larger than they are (at most 2^14): fp16 has no 11 bits below 2^-14, and no second part.
 constexpr float kCeExpBits = 14.f;
 
+// What a K block's stage holds, and whether the accumulator is emptied in rounds.
+enum GemmMode {
+  GEMM_ONE = 0,      // one plane of each operand
+  GEMM_LOW = 1,      // a low part of one operand, too
+  GEMM_SPLIT = 2,    // both parts of both, in rounds
+};
+
 // kPair: tiles of 256 x 256 on CTA pairs, else 128 x 128 on single CTAs.
-template <int kEpi, bool kPair, bool kRounds>
+template <int kEpi, bool kPair, int kMode>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ GemmParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  float* scratch_all = reinterpret_cast<float*>(smem + kGemmStages * kGemmStageBytes);
+  float* scratch_all = reinterpret_cast<float*>(smem + kGemmRingBytes);
   GemmTail* tail = reinterpret_cast<GemmTail*>(scratch_all + kGemmEpiWarps * kGemmScratchFloats);
   volatile int* abort_flag = &tail->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -291,8 +375,12 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t tmem_base = tail->tmem_base;
-  const int steps = p.kblocks * p.nseg;
+  const int steps = p.kblocks;
+  constexpr bool kRounds = kMode == GEMM_SPLIT;
   const int round_len = kRounds ? p.round_len : steps;
+  constexpr uint32_t kTiles = 2 + kMode, kStages = 12 / kTiles, kStageBytes = kTiles * kGemmTileBytes;
+  // (GEMM_LOW: which operand has two parts is known at run time)
+  const int a_planes = kMode == GEMM_SPLIT ? 2 : (kMode == GEMM_LOW ? p.a_planes : 1);
   bool failed = false;
 
   if (warp == 0) {
@@ -301,48 +389,37 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       int b, tm, tn;
       gemm_tile(p, t, b, tm, tn);
       const int m0 = tm * kTileM + (int)rank * 128, n0 = tn * kTileN + (int)rank * 128;
-      int kb = 0, seg = 0;
       for (int i = 0; i < steps; ++i) {
         if (!mbar_wait_warp(&tail->empty[s], ph ^ 1, abort_flag)) { failed = true; break; }
         if (elect_one()) {
-          uint8_t* pa = smem + s * kGemmStageBytes;
-          uint8_t* pb = pa + 16384;
-          const int az = p.a_z[seg] + b, bz = p.b_z[seg] + b, k0 = kb * 64;
-          if constexpr (kPair) {
-            const uint32_t fb = mapa_u32(smem_u32(&tail->full[s]), 0);
-            if (leader) mbar_expect_tx(&tail->full[s], 2 * kGemmStageBytes);
-            if (p.a_mn) {
-              tma2_load_3d(pa, &tmA, fb, m0, k0, az);
-              tma2_load_3d(pa + 8192, &tmA, fb, m0 + 64, k0, az);
+          uint8_t* dst = smem + s * kStageBytes;
+          const int k0 = i * 64;
+          uint64_t* full = &tail->full[s];
+          const uint32_t fb = kPair ? mapa_u32(smem_u32(full), 0) : 0;
+          if (leader) mbar_expect_tx(full, kCtas * kStageBytes);
+#pragma unroll
+          for (int x = 0; x < (int)kTiles; ++x) {
+            const bool is_a = x < a_planes;
+            const CUtensorMap* map = is_a ? &tmA : &tmB;
+            const int r0 = is_a ? m0 : n0, z = (is_a ? x : x - a_planes) * p.batch + b;
+            // rows contiguous: two boxes of 64 rows by 64 K; K contiguous: one of 128 rows
+            if (is_a ? p.a_mn : p.b_mn) {
+              if constexpr (kPair) {
+                tma2_load_3d(dst, map, fb, r0, k0, z);
+                tma2_load_3d(dst + 8192, map, fb, r0 + 64, k0, z);
+              } else {
+                tma_load_3d(dst, map, full, r0, k0, z);
+                tma_load_3d(dst + 8192, map, full, r0 + 64, k0, z);
+              }
             } else {
-              tma2_load_3d(pa, &tmA, fb, k0, m0, az);
+              if constexpr (kPair) tma2_load_3d(dst, map, fb, k0, r0, z);
+              else tma_load_3d(dst, map, full, k0, r0, z);
             }
-            if (p.b_mn) {
-              tma2_load_3d(pb, &tmB, fb, n0, k0, bz);
-              tma2_load_3d(pb + 8192, &tmB, fb, n0 + 64, k0, bz);
-            } else {
-              tma2_load_3d(pb, &tmB, fb, k0, n0, bz);
-            }
-          } else {
-            uint64_t* fb = &tail->full[s];
-            mbar_expect_tx(fb, kGemmStageBytes);
-            if (p.a_mn) {
-              tma_load_3d(pa, &tmA, fb, m0, k0, az);
-              tma_load_3d(pa + 8192, &tmA, fb, m0 + 64, k0, az);
-            } else {
-              tma_load_3d(pa, &tmA, fb, k0, m0, az);
-            }
-            if (p.b_mn) {
-              tma_load_3d(pb, &tmB, fb, n0, k0, bz);
-              tma_load_3d(pb + 8192, &tmB, fb, n0 + 64, k0, bz);
-            } else {
-              tma_load_3d(pb, &tmB, fb, k0, n0, bz);
-            }
+            dst += kGemmTileBytes;
           }
         }
         __syncwarp();
-        if (++s == kGemmStages) { s = 0; ph ^= 1; }
-        if (++seg == p.nseg) { seg = 0; ++kb; }
+        if (++s == kStages) { s = 0; ph ^= 1; }
       }
     }
   } else if (warp == 1 && leader) {
@@ -365,15 +442,30 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           for (int i = i0; i < i1; ++i) {
             if (!mbar_wait_hot(&tail->full[s], ph, abort_flag)) { failed = true; break; }
             tc_fence_after();
-            const uint64_t ad = smem_desc(da, base + s * kGemmStageBytes), bd = smem_desc(db, base + s * kGemmStageBytes + 16384);
+            const uint32_t at = base + s * kStageBytes;
+            auto product = [&](int x, int y, uint32_t more) {   // tiles x (of A) and y (of B) of the stage
+              const uint64_t ad = smem_desc(da, at + x * kGemmTileBytes), bd = smem_desc(db, at + y * kGemmTileBytes);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if constexpr (kPair) mma2_bf16(d, ad + (uint64_t)(j * ka), bd + (uint64_t)(j * kb16), p.idesc, (i > i0 || j) ? 1u : 0u);
-              else mma_bf16(d, ad + (uint64_t)(j * ka), bd + (uint64_t)(j * kb16), p.idesc, (i > i0 || j) ? 1u : 0u);
+              for (int j = 0; j < 4; ++j) {
+                if constexpr (kPair) mma2_bf16(d, ad + (uint64_t)(j * ka), bd + (uint64_t)(j * kb16), p.idesc, j ? 1u : more);
+                else mma_bf16(d, ad + (uint64_t)(j * ka), bd + (uint64_t)(j * kb16), p.idesc, j ? 1u : more);
+              }
+            };
+            // low parts first: the accumulator is cut off at each step, by less while it is small
+            const uint32_t more = i > i0 ? 1u : 0u;
+            if constexpr (kMode == GEMM_SPLIT) {
+              product(0, 3, more);
+              product(1, 2, 1u);
+              product(0, 2, 1u);
+            } else if constexpr (kMode == GEMM_LOW) {
+              product(a_planes - 1, 2, more);
+              product(0, a_planes == 2 ? 2 : 1, 1u);
+            } else {
+              product(0, 1, more);
             }
             if constexpr (kPair) mma2_commit_both(&tail->empty[s]);
             else mma_commit(&tail->empty[s]);
-            if (++s == kGemmStages) { s = 0; ph ^= 1; }
+            if (++s == kStages) { s = 0; ph ^= 1; }
           }
           if (failed) break;
           if constexpr (kPair) mma2_commit_both(&tail->tmem_full[buf]);
@@ -403,18 +495,19 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
           for (int j = 0; j < 32; ++j) acc[g][j] = 0.f;
       }
-      for (int i0 = 0; i0 < steps; i0 += round_len) {
+      uint32_t taddr;
+      auto release = [&] {   // everything of this accumulator has been read
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (kPair) mbar_arrive_cluster(mapa_u32(smem_u32(&tail->tmem_empty[buf]), 0));
+          else mbar_arrive(&tail->tmem_empty[buf]);
+        }
+      };
+      for (int i0 = 0;; i0 += round_len) {
         if (!mbar_wait_warp(&tail->tmem_full[buf], bph, abort_flag)) { failed = true; break; }
         tc_fence_after();
-        const uint32_t taddr = tmem_base + buf * kAccCols + half * (kTileN / 2) + ((uint32_t)(q * 32) << 16);
-        auto release = [&] {   // everything of this accumulator has been read
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if constexpr (kPair) mbar_arrive_cluster(mapa_u32(smem_u32(&tail->tmem_empty[buf]), 0));
-            else mbar_arrive(&tail->tmem_empty[buf]);
-          }
-        };
+        taddr = tmem_base + buf * kAccCols + half * (kTileN / 2) + ((uint32_t)(q * 32) << 16);
         if constexpr (kRounds) {
 #pragma unroll
           for (int g = 0; g < kGroups; ++g) {
@@ -423,85 +516,68 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
             for (int j = 0; j < 32; ++j) acc[g][j] += v[j];
           }
-          release();
         }
-        if (!kRounds || i0 + round_len >= steps) {
-          if constexpr (kEpi == EPI_CE) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-              float v[32];
-              if constexpr (!kRounds) tmem_ld32(taddr + g * 32, v);
-              else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = acc[g][j];
-              }
-              ce_logits(p, col0 + g * 32, f, lane, v);
-#pragma unroll
-              for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
-            }
-            const float ref = top == -INFINITY ? 0.f : top;   // a half without any class counts nothing
-            const int label = row < p.M ? p.labels[row] : -1;
-            float sum = 0.f;
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-              const int col = col0 + g * 32;
-              float v[32];
-              if constexpr (!kRounds) tmem_ld32(taddr + g * 32, v);
-              else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = acc[g][j];
-              }
-              if constexpr (!kRounds) {
-                if (g + 1 == kGroups) release();
-              }
-              ce_logits(p, col, f, lane, v);
-              if (label >= col && label < col + 32) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                  if (col + j == label) p.target[row] = v[j];
-              }
-#pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                v[j] = exp2f(fmaf(v[j] - ref, kLog2e, kCeExpBits));
-                sum += v[j];
-              }
-              if (p.h_out && row < p.M && col < p.N) {
-                __half* dst = p.h_out + (long long)row * p.h_ld + col;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                  __half hi[8], lo[8];
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) split_half(v[8 * u + j], hi[j], lo[j]);
-                  *reinterpret_cast<uint4*>(dst + 8 * u) = make_uint4(pack_half2(hi[0], hi[1]), pack_half2(hi[2], hi[3]),
-                                                                      pack_half2(hi[4], hi[5]), pack_half2(hi[6], hi[7]));
-                  if (kRounds)
-                    *reinterpret_cast<uint4*>(dst + p.h_plane + 8 * u) = make_uint4(pack_half2(lo[0], lo[1]), pack_half2(lo[2], lo[3]),
-                                                                                    pack_half2(lo[4], lo[5]), pack_half2(lo[6], lo[7]));
-                }
-              }
-            }
-            if (row < p.M) p.stats[(long long)(tn * 2 + half) * p.stats_ld + row] = make_float2(ref, sum * 6.103515625e-5f);
-          } else {
-            const bool mirror = p.sym && tm != tn;
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-              float v[32];
-              if constexpr (!kRounds) {
-                tmem_ld32(taddr + g * 32, v);
-                if (g + 1 == kGroups) release();
-              } else {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = acc[g][j];
-              }
-              if constexpr (kEpi == EPI_H16) epi_h16(p, b, row, col0 + g * 32, mirror, f, v);
-              else epi_out(p, b, row0, col0 + g * 32, f, v, scratch, lane);
-            }
-          }
-        }
+        if (i0 + round_len >= steps) break;
+        release();
         buf ^= 1;
         if (!buf) bph ^= 1;
       }
+      if (failed) break;
+      if constexpr (kRounds) {   // the sum goes back to where the accumulator was: what follows reads it group by group
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) tmem_st32(taddr + g * 32, acc[g]);
+      }
+      if constexpr (kEpi == EPI_CE) {
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int g = 0; g < kGroups; ++g) {
+          float v[32];
+          tmem_ld32(taddr + g * 32, v);
+          ce_logits(p, col0 + g * 32, f, lane, v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
+        }
+        const float ref = top == -INFINITY ? 0.f : top;   // a half without any class counts nothing
+        const int label = row < p.M ? p.labels[row] : -1;
+        float sum = 0.f;
+#pragma unroll 1
+        for (int g = 0; g < kGroups; ++g) {
+          const int col = col0 + g * 32;
+          float v[32];
+          tmem_ld32(taddr + g * 32, v);
+          if (g + 1 == kGroups) release();
+          ce_logits(p, col, f, lane, v);
+          if (label >= col && label < col + 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (col + j == label) p.target[row] = v[j];
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            v[j] = exp2f(fmaf(v[j] - ref, kLog2e, kCeExpBits));
+            sum += v[j];
+          }
+          if (p.h_out && col < p.N) epi_h16(p, 0, row, col, false, v);
+        }
+        if (row < p.M) p.stats[(long long)(tn * 2 + half) * p.stats_ld + row] = make_float2(ref, sum * 6.103515625e-5f);
+      } else {
+        const bool mirror = p.sym && tm != tn;
+#pragma unroll 1
+        for (int g = 0; g < kGroups; ++g) {
+          const int col = col0 + g * 32;
+          float v[32];
+          tmem_ld32(taddr + g * 32, v);
+          if (g + 1 == kGroups) release();
+          if (col >= p.N) continue;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] *= f;
+          if constexpr (kEpi == EPI_H16) epi_h16(p, b, row, col, mirror, v);
+          else if (p.out_vec) epi_out_vec(p, b, row, col, v);
+          else epi_out_any(p, b, row0, col, v, scratch, lane);
+        }
+      }
+      buf ^= 1;
+      if (!buf) bph ^= 1;
     }
   }
 

@@ -94,7 +94,9 @@ __device__ __forceinline__ float ce_scale_of(float amax) {
 
 // The operands as the products take them, rows `ld` apart: fp32 as fp16 high and low parts of the scaled values, bf16 as it is.
 // Rows of x whose label is no class become zeros: what stands there (padding, NaN) must not reach dw through a product with 0.
-// Blocks [0, xb) take x, the rest w (none where it is used in place).  The first block writes the header's scales.
+// Blocks [0, xb) take x, the rest w (none where it is used in place).  The first block writes the header's scales.  kVec: D is a
+// multiple of 8.
+template <bool kVec>
 __global__ void __launch_bounds__(kCeThreads)
 ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int32_t* __restrict__ labels, int is_bf16, int T, int D, int V,
                long long ld, __half* __restrict__ xo, long long x_plane, __half* __restrict__ wo, long long w_plane, int xb,
@@ -129,31 +131,60 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int
   __half* dst = of_w ? wo : xo;
   const long long plane = of_w ? w_plane : x_plane;
   const float scale = scales[of_w];
-  const long long n = (long long)(of_w ? V : T) * D;
+  constexpr int N = kVec ? 8 : 1;
+  const int per_row = D / N;
+  const long long n = (long long)(of_w ? V : T) * per_row;
+#pragma unroll 2
   for (long long i = (long long)blk * kCeThreads + threadIdx.x; i < n; i += (long long)blks * kCeThreads) {
-    const long long r = i / D, at = r * ld + (i - r * D);
+    const long long r = n >> 32 ? i / per_row : (long long)((uint32_t)i / (uint32_t)per_row);
+    const long long from = i * N, at = r * ld + (i - r * per_row) * N;
     const bool keep = of_w || ce_counts(labels[r], V);
     if (is_bf16) {
-      ((bf16*)dst)[at] = keep ? ((const bf16*)src)[i] : __float2bfloat16_rn(0.f);
+      if constexpr (kVec) {
+        uint4 v = ld_raw((const bf16*)src + from);
+        if (!keep) v = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>((bf16*)dst + at) = v;
+      } else {
+        ((bf16*)dst)[at] = keep ? ((const bf16*)src)[from] : __float2bfloat16_rn(0.f);
+      }
     } else {
-      __half hi, lo;
-      tc::split_half(keep ? ((const float*)src)[i] * scale : 0.f, hi, lo);
-      dst[at] = hi;
-      dst[plane + at] = lo;
+      __half hi[N], lo[N];
+      float v[N];
+      if constexpr (kVec) {
+        float a[4], b[4];
+        ldv((const float*)src + from, a);
+        ldv((const float*)src + from + 4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[4 + j] = b[j]; }
+      } else {
+        v[0] = ((const float*)src)[from];
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) tc::split_half(keep ? v[j] * scale : 0.f, hi[j], lo[j]);
+      if constexpr (kVec) {
+        *reinterpret_cast<uint4*>(dst + at) = make_uint4(tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]),
+                                                         tc::pack_half2(hi[4], hi[5]), tc::pack_half2(hi[6], hi[7]));
+        *reinterpret_cast<uint4*>(dst + plane + at) = make_uint4(tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]),
+                                                                 tc::pack_half2(lo[4], lo[5]), tc::pack_half2(lo[6], lo[7]));
+      } else {
+        dst[at] = hi[0];
+        dst[plane + at] = lo[0];
+      }
     }
   }
 }
 
-// lse and loss of each row from its parts: 32 rows a block, 8 threads a row.
+// lse and loss of each row from its parts: 8 rows a block (32 bytes of each part), 32 threads a row.
 __global__ void __launch_bounds__(kCeThreads)
 ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, int rows, int V, const int32_t* __restrict__ labels,
                const float* __restrict__ target, float* __restrict__ lse, float* __restrict__ row_loss) {
   pdl_wait();
   pdl_launch_dependents();
-  const int r = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * 32 + r;
+  const int r = threadIdx.x & 7, y = threadIdx.x >> 3, row = blockIdx.x * 8 + r;
   float m = -INFINITY, s = 0.f;
-  if (row < rows)
-    for (int i = y; i < parts; i += 8) {
+  if (row < rows) {
+#pragma unroll 4
+    for (int i = y; i < parts; i += 32) {
       const float2 v = stats[(long long)i * stats_ld + row];
       if (v.y == 0.f) continue;              // a part without any class (its reference says nothing)
       const float top = fmaxf(m, v.x);
@@ -161,14 +192,15 @@ ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, 
       s = s * exp2f((m - top) * tc::kLog2e) + v.y * exp2f((v.x - top) * tc::kLog2e);
       m = top;
     }
-  __shared__ float ms[8][32], ss[8][32];
+  }
+  __shared__ float ms[32][8], ss[32][8];
   ms[y][r] = m;
   ss[y][r] = s;
   __syncthreads();
   if (y || row >= rows) return;
-  for (int i = 1; i < 8; ++i) m = fmaxf(m, ms[i][r]);
+  for (int i = 1; i < 32; ++i) m = fmaxf(m, ms[i][r]);
   float sum = 0.f;
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 32; ++i)
     if (ss[i][r] != 0.f) sum += ss[i][r] * exp2f((ms[i][r] - m) * tc::kLog2e);
   const float l = m + logf(sum);
   lse[row] = l;

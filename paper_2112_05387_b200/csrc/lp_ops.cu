@@ -64,18 +64,6 @@ size_t ortho_scratch_bytes(int batch, int rows, int cols, bool split) {
   return c.off;
 }
 
-// Segments of a product of operands kept in `pa` and `pb` planes of `count` matrices each: all products of parts but lo * lo.
-static void gemm_segments(tc::GemmParams& p, int pa, int pb, int count) {
-  p.nseg = 0;
-  for (int i = 0; i < pa; ++i)
-    for (int j = 0; j < pb; ++j) {
-      if (i && j) continue;
-      p.a_z[p.nseg] = i * count;
-      p.b_z[p.nseg] = j * count;
-      ++p.nseg;
-    }
-}
-
 int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* launches) {
   int rc = gemm_init_dev();
   if (rc != LP_OK) return rc;
@@ -98,9 +86,12 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   }
   // bf16 gradients are exact in one plane; a momentum or an fp32 gradient is not
   int x_planes = (q.g_bf16 && !q.momentum && !q.split) ? 1 : 2;
-  LP_CUDA_OK(launch_pdl(ortho_norm_kernel, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts, s.sums, s.err));
-  LP_CUDA_OK(launch_pdl(ortho_pack_kernel, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts, (const double*)s.sums, q.eps, q.cols,
-                        s.ld, s.x[0], x_mat, x_planes == 2 ? x_plane : 0LL, s.alpha));
+  bool vec = q.cols % 8 == 0;
+  for (int b = 0; q.off && b < B; ++b) vec = vec && q.off[b] % 8 == 0;
+  LP_CUDA_OK(launch_pdl(vec ? ortho_norm_kernel<true> : ortho_norm_kernel<false>, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts,
+                        s.sums, s.err));
+  LP_CUDA_OK(launch_pdl(vec ? ortho_pack_kernel<true> : ortho_pack_kernel<false>, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts,
+                        (const double*)s.sums, q.eps, q.cols, s.ld, s.x[0], x_mat, x_planes == 2 ? x_plane : 0LL, s.alpha));
   n += 2;
 
   // tensor maps, once a call: X in both buffers and both orders, A and B with K contiguous (they are symmetric)
@@ -122,29 +113,29 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     tc::GemmParams p;
     memset(&p, 0, sizeof(p));
     p.M = p.N = small; p.batch = B; p.sym = 1; p.err = s.err;
-    gemm_segments(p, planes, planes, B);
+    p.a_planes = p.b_planes = planes;
     p.f = first ? kScaleA : kScaleA / (kScaleX * kScaleX);
     p.f_dev = s.alpha; p.f_pow = first ? 2 : 0;
     p.h_out = s.a; p.h_ld = s.ld_s; p.h_batch = s_mat; p.h_plane = q.split ? s_plane : 0;
-    if (tall) rc = launch_gemm<tc::EPI_H16>(p, q.rows, m_xm[cur], true, m_xm[cur], true, false, q.split, pair_s, st);
-    else rc = launch_gemm<tc::EPI_H16>(p, q.cols, m_xk[cur], false, m_xk[cur], false, false, q.split, pair_s, st);
+    if (tall) rc = launch_gemm<tc::EPI_H16>(p, q.rows, m_xm[cur], true, m_xm[cur], true, false, pair_s, st);
+    else rc = launch_gemm<tc::EPI_H16>(p, q.cols, m_xk[cur], false, m_xk[cur], false, false, pair_s, st);
     if (rc != LP_OK) return rc;
     // B = a I + b A + c A^2
     memset(&p, 0, sizeof(p));
     p.M = p.N = small; p.batch = B; p.sym = 1; p.err = s.err;
-    gemm_segments(p, planes, planes, B);
+    p.a_planes = p.b_planes = planes;
     p.f = q.coeffs[2] * (kScaleB / (kScaleA * kScaleA));
     p.h_out = s.b; p.h_ld = s.ld_s; p.h_batch = s_mat; p.h_plane = q.split ? s_plane : 0;
     p.aux = s.a; p.aux_f = q.coeffs[1] * (kScaleB / kScaleA); p.diag = q.coeffs[0] * kScaleB;
-    rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, q.split, pair_s, st);
+    rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, pair_s, st);
     if (rc != LP_OK) return rc;
     // X <- B X (X B).  An error in X grows by up to a in each later step, so its low part is kept while three or more
     // products follow (relative error of the result, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3 with the
     // low parts of two steps, 1.1e-3 with all; fp16's step in A and B costs 1e-3)
     memset(&p, 0, sizeof(p));
     p.M = q.rows; p.N = q.cols; p.batch = B; p.err = s.err;
-    if (tall) gemm_segments(p, x_planes, planes, B);
-    else gemm_segments(p, planes, x_planes, B);
+    p.a_planes = tall ? x_planes : planes;
+    p.b_planes = tall ? planes : x_planes;
     p.f = last ? 1.f / (first ? kScaleB : kScaleB * kScaleX) : (first ? kScaleX / kScaleB : 1.f / kScaleB);
     p.f_dev = s.alpha; p.f_pow = first ? 1 : 0;
     const CUtensorMap& ma = tall ? m_xk[cur] : m_b;
@@ -156,12 +147,12 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
         p.use_off = 1;
         for (int b = 0; b < B; ++b) p.off[b] = q.off[b];
       }
-      rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, q.split, pair_x, st);
+      rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, pair_x, st);
     } else {
       x_planes = (q.split || i + 3 < q.steps) ? 2 : 1;
       cur ^= 1;
       p.h_out = s.x[cur]; p.h_ld = s.ld; p.h_batch = x_mat; p.h_plane = x_planes == 2 ? x_plane : 0;
-      rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, q.split, pair_x, st);
+      rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, pair_x, st);
     }
     if (rc != LP_OK) return rc;
     n += 3;
@@ -183,7 +174,9 @@ static int check_ortho(int dtype, int batch, int rows, int cols, int steps, floa
 // ---------------------------------------------------------------------------------------------
 // loss of a linear layer
 // ---------------------------------------------------------------------------------------------
-static const size_t kCePieceBytes = (size_t)512 << 20;   // exponentials of a piece of rows
+// Exponentials of a piece of rows: 512 MB, or as much as the fp32 sums of dw over several pieces would take, if that makes it
+// one piece.
+static const size_t kCePieceBytes = (size_t)512 << 20;
 static const int kCeAmaxParts = 592;
 
 struct CeScratch {
@@ -205,7 +198,8 @@ static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) 
   s.ld_d = (D + 7) / 8 * 8;
   // (the loss alone keeps 16 bytes for each row and 128 classes)
   const size_t row_bytes = grads ? (size_t)s.ld_v * 2 * planes : (size_t)((V + 127) / 128) * 16;
-  const long long fit = (long long)(kCePieceBytes / row_bytes) / 256 * 256;
+  const bool whole = grads && !s.f32 && (size_t)T * row_bytes <= (size_t)V * D * 4;
+  const long long fit = whole ? T : (long long)(kCePieceBytes / row_bytes) / 256 * 256;
   s.rows = (int)std::min<long long>(T, std::min(std::max(256LL, fit), 1LL << 18));
   // rows of a block of the pass over the exponentials: 64, fewer where that leaves SMs idle
   s.slab = 64;
@@ -308,7 +302,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   if (s.x) {
     const int xb = grid_for((long long)T * D, kCeThreads * 8, Dv.sm_count, 4);
     const int wb = s.w ? grid_for((long long)V * D, kCeThreads * 8, Dv.sm_count, 8) : 0;
-    LP_CUDA_OK(launch_pdl(ce_pack_kernel, dim3(xb + wb), dim3(kCeThreads), 0, st, x, w, labels, is_bf16, T, D, V, s.ld_d, s.x, x_plane, s.w,
+    LP_CUDA_OK(launch_pdl(D % 8 ? ce_pack_kernel<false> : ce_pack_kernel<true>, dim3(xb + wb), dim3(kCeThreads), 0, st, x, w, labels, is_bf16, T, D, V, s.ld_d, s.x, x_plane, s.w,
                           w_plane, xb, (const float*)s.amax, kCeAmaxParts, grad_scale, s.hdr));
   }
   const void* xm = s.x ? (const void*)s.x : x;
@@ -329,13 +323,13 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     tc::GemmParams p;
     memset(&p, 0, sizeof(p));
     p.M = rows; p.N = V; p.batch = 1; p.err = &s.hdr->err;
-    gemm_segments(p, planes, planes, 1);
+    p.a_planes = p.b_planes = planes;
     p.f = 1.f; p.f_dev = &s.hdr->logit_f; p.f_pow = s.f32 ? 1 : 0;
     p.bias = bias; p.bias_bf16 = is_bf16; p.labels = labels + r0;
     p.stats = s.stats; p.stats_ld = s.rows; p.target = s.target + r0;
     p.h_out = s.p; p.h_ld = s.ld_v; p.h_plane = s.f32 ? p_plane : 0;
-    if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, s.f32, pair, st)) != LP_OK) return rc;
-    LP_CUDA_OK(launch_pdl(ce_rows_kernel, dim3((rows + 31) / 32), dim3(kCeThreads), 0, st, (const float2*)s.stats, (long long)s.rows, parts,
+    if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, pair, st)) != LP_OK) return rc;
+    LP_CUDA_OK(launch_pdl(ce_rows_kernel, dim3((rows + 7) / 8), dim3(kCeThreads), 0, st, (const float2*)s.stats, (long long)s.rows, parts,
                           rows, V, labels + r0, (const float*)(s.target + r0), s.lse + r0, rl + r0));
     if (!grads) continue;
     const int slabs = (rows + s.slab - 1) / s.slab;
@@ -350,18 +344,18 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       if ((rc = encode_gemm_map(&m_pk, op, false)) != LP_OK) return rc;
       memset(&p, 0, sizeof(p));
       p.M = rows; p.N = D; p.batch = 1; p.err = &s.hdr->err;
-      gemm_segments(p, planes, planes, 1);
+      p.a_planes = p.b_planes = planes;
       p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1;
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
       const bool pr = gemm_pair_tiles(rows, D, 1, false, Dv.sm_count, Dv.gemm_pairs);
-      if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, s.f32, pr, st)) != LP_OK) return rc;
+      if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, pr, st)) != LP_OK) return rc;
     }
     if (dw) {
       if ((rc = encode_gemm_map(&m_pm, op, true)) != LP_OK) return rc;
       if ((rc = encode_gemm_map(&m_xm, ox, true)) != LP_OK) return rc;
       memset(&p, 0, sizeof(p));
       p.M = V; p.N = D; p.batch = 1; p.err = &s.hdr->err;
-      gemm_segments(p, planes, planes, 1);
+      p.a_planes = p.b_planes = planes;
       p.f = 1.f; p.f_dev = &s.hdr->dw_f; p.f_pow = 1;
       p.out = dw; p.out_bf16 = is_bf16; p.out_ld = D;
       if (s.rows < T) {
@@ -370,7 +364,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
         p.acc_last = r0 + rows == T;
       }
       const bool pr = gemm_pair_tiles(V, D, 1, false, Dv.sm_count, Dv.gemm_pairs);
-      if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, s.f32, pr, st)) != LP_OK) return rc;
+      if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, pr, st)) != LP_OK) return rc;
     }
   }
   if (dbias)

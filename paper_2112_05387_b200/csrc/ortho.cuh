@@ -16,7 +16,7 @@
 namespace lp {
 
 constexpr int kOrthoThreads = 256;
-constexpr int kOrthoMaxParts = 512;
+constexpr int kOrthoMaxParts = 1184;
 
 struct OrthoSource {
   const void* g;          // gradients, fp32 or bf16, contiguous matrices
@@ -29,31 +29,71 @@ struct OrthoSource {
   long long off[tc::kGemmMaxOffsets];
 };
 
-__device__ __forceinline__ float ortho_grad(const OrthoSource& s, long long i) {
-  return s.g_bf16 ? __bfloat162float(((const bf16*)s.g)[i]) : ((const float*)s.g)[i];
+// kVec: eight elements at a time (columns and offsets are multiples of 8), else one.
+template <bool kVec>
+struct OrthoVec {
+  static constexpr int N = kVec ? 8 : 1;
+};
+template <bool kVec>
+__device__ __forceinline__ void ortho_load(const void* p, int is_bf16, long long i, float (&v)[OrthoVec<kVec>::N]) {
+  if constexpr (kVec) {
+    if (is_bf16) {
+      ldv((const bf16*)p + i, v);
+    } else {
+      float a[4], b[4];
+      ldv((const float*)p + i, a);
+      ldv((const float*)p + i + 4, b);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[4 + j] = b[j]; }
+    }
+  } else {
+    v[0] = is_bf16 ? __bfloat162float(((const bf16*)p)[i]) : ((const float*)p)[i];
+  }
+}
+template <bool kVec>
+__device__ __forceinline__ void ortho_store(float* p, long long i, const float (&v)[OrthoVec<kVec>::N]) {
+  if constexpr (kVec) {
+    *reinterpret_cast<float4*>(p + i) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(p + i + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    p[i] = v[0];
+  }
+}
+// What is orthogonalised, from the gradient and the momentum after its update.
+template <int N>
+__device__ __forceinline__ void ortho_direction(const OrthoSource& s, float (&g)[N], const float (&m)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) g[j] = s.nesterov ? fmaf(s.mu, m[j], g[j]) : m[j];
 }
 
-// Sums of squares of what is orthogonalised, `parts` partial sums a matrix; the momentum is updated on the way:
+// Sums of squares of what is orthogonalised, `parts` partial sums a matrix, in fp64 (a gradient of 1e-25 or 1e25 squares out of
+// fp32's range); the momentum is updated on the way:
 //   m <- mu m + g;  u = m, or g + mu m (Nesterov).
+template <bool kVec>
 __global__ void __launch_bounds__(kOrthoThreads)
 ortho_norm_kernel(const __grid_constant__ OrthoSource s, int parts, double* __restrict__ sums, int* __restrict__ err) {
+  constexpr int N = OrthoVec<kVec>::N;
   pdl_wait();
   pdl_launch_dependents();
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *err = 0;
   const int b = blockIdx.y;
-  const long long base = s.use_off ? s.off[b] : b * s.elems;
-  const long long lo = s.elems * blockIdx.x / parts, hi = s.elems * (blockIdx.x + 1) / parts;
+  const long long base = s.use_off ? s.off[b] : b * s.elems, groups = s.elems / N;
+  const long long lo = groups * blockIdx.x / parts, hi = groups * (blockIdx.x + 1) / parts;
   double sum = 0.0;
-#pragma unroll 4
+#pragma unroll 2
   for (long long i = lo + threadIdx.x; i < hi; i += kOrthoThreads) {
-    float u = ortho_grad(s, base + i);
+    float u[N];
+    ortho_load<kVec>(s.g, s.g_bf16, base + i * N, u);
     if (s.momentum) {
-      const float g = u;
-      const float m = fmaf(s.mu, s.momentum[base + i], g);
-      s.momentum[base + i] = m;
-      u = s.nesterov ? fmaf(s.mu, m, g) : m;
+      float m[N];
+      ortho_load<kVec>(s.momentum, 0, base + i * N, m);
+#pragma unroll
+      for (int j = 0; j < N; ++j) m[j] = fmaf(s.mu, m[j], u[j]);
+      ortho_store<kVec>(s.momentum, base + i * N, m);
+      ortho_direction(s, u, m);
     }
-    sum += (double)u * (double)u;
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum += (double)u[j] * (double)u[j];
   }
   __shared__ double part[kOrthoThreads / 32];
 #pragma unroll
@@ -66,41 +106,66 @@ ortho_norm_kernel(const __grid_constant__ OrthoSource s, int parts, double* __re
   }
 }
 
-// fp16 planes of u 2^k (rows `ld` apart), and alpha = 1 / (max(norm, eps) 2^k) of each matrix.
+// Scale 2^k of a matrix's planes and alpha = 1 / (max(norm, eps) 2^k), from the partial sums of squares; by one warp.
+__device__ __forceinline__ void ortho_scale(const double* sums, int parts, float eps, float& scale, float& alpha) {
+  double sum = 0.0;
+  for (int i = threadIdx.x & 31; i < parts; i += 32) sum += sums[i];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const double norm = fmax(sqrt(sum), (double)eps);
+  const int k = isfinite(norm) ? 14 - ilogb(norm) : 0;
+  scale = (float)ldexp(1.0, k);
+  alpha = (float)(1.0 / ldexp(norm, k));
+}
+
+// fp16 planes of u 2^k (rows `ld` apart), and alpha.
+template <bool kVec>
 __global__ void __launch_bounds__(kOrthoThreads)
 ortho_pack_kernel(const __grid_constant__ OrthoSource s, int parts, const double* __restrict__ sums, float eps, int cols, long long ld,
                   __half* __restrict__ x, long long x_batch, long long x_plane /* 0: no low part */, float* __restrict__ alpha) {
+  constexpr int N = OrthoVec<kVec>::N;
   pdl_wait();
   pdl_launch_dependents();
   const int b = blockIdx.y;
   __shared__ float scale_s;
   if (threadIdx.x < 32) {
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < parts; i += 32) sum += sums[(long long)b * parts + i];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    float sc, al;
+    ortho_scale(sums + (long long)b * parts, parts, eps, sc, al);
     if (threadIdx.x == 0) {
-      const double norm = fmax(sqrt(sum), (double)eps);
-      const int k = isfinite(norm) ? 14 - ilogb(norm) : 0;
-      scale_s = (float)ldexp(1.0, k);
-      if (blockIdx.x == 0) alpha[b] = (float)(1.0 / ldexp(norm, k));
+      scale_s = sc;
+      if (blockIdx.x == 0) alpha[b] = al;
     }
   }
   __syncthreads();
   const float scale = scale_s;
-  const long long base = s.use_off ? s.off[b] : b * s.elems;
+  const long long base = s.use_off ? s.off[b] : b * s.elems, groups = s.elems / N;
+  const int per_row = cols / N;
   __half* out = x + b * x_batch;
-  for (long long i = (long long)blockIdx.x * kOrthoThreads + threadIdx.x; i < s.elems; i += (long long)gridDim.x * kOrthoThreads) {
-    float u = ortho_grad(s, base + i);
+#pragma unroll 2
+  for (long long i = (long long)blockIdx.x * kOrthoThreads + threadIdx.x; i < groups; i += (long long)gridDim.x * kOrthoThreads) {
+    float u[N];
+    ortho_load<kVec>(s.g, s.g_bf16, base + i * N, u);
     if (s.momentum) {
-      const float m = s.momentum[base + i];
-      u = s.nesterov ? fmaf(s.mu, m, u) : m;
+      float m[N];
+      ortho_load<kVec>(s.momentum, 0, base + i * N, m);
+      ortho_direction(s, u, m);
     }
-    __half hi, lo;
-    tc::split_half(u * scale, hi, lo);
-    const long long r = i / cols, at = r * ld + (i - r * cols);
-    out[at] = hi;
-    if (x_plane) out[x_plane + at] = lo;
+    __half hi[N], lo[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) tc::split_half(u[j] * scale, hi[j], lo[j]);
+    // (a 64-bit division costs as much as the rest of the loop)
+    const long long r = groups >> 32 ? i / per_row : (long long)((uint32_t)i / (uint32_t)per_row);
+    __half* at = out + r * ld + (i - r * per_row) * N;
+    if constexpr (kVec) {
+      *reinterpret_cast<uint4*>(at) = make_uint4(tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]), tc::pack_half2(hi[4], hi[5]),
+                                                 tc::pack_half2(hi[6], hi[7]));
+      if (x_plane)
+        *reinterpret_cast<uint4*>(at + x_plane) = make_uint4(tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]),
+                                                             tc::pack_half2(lo[4], lo[5]), tc::pack_half2(lo[6], lo[7]));
+    } else {
+      *at = hi[0];
+      if (x_plane) at[x_plane] = lo[0];
+    }
   }
 }
 
