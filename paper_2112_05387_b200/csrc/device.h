@@ -34,7 +34,7 @@ struct Device {
   EncodeTiledFn encode = nullptr;
   // kernel attributes are per device: set on the first launch of each kernel family on that device
   bool conv_attr = false, wgrad_attr = false, wgrad_halo_attr = false, conv2_attr = false, f32_attr = false, thin_attr = false,
-       gemm_attr = false;
+       gemm_attr = false, ortho_attr = false;
   int max_pairs = 0;   // CTA pairs of conv_tc2_kernel that can be resident at once (0: not usable)
   int gemm_pairs = 0;  // the same for gemm_tc_kernel
   int init() {

@@ -65,15 +65,19 @@ static int gemm_init_dev() {
   return LP_OK;
 }
 
-// Tiles of 256 x 256 on CTA pairs, or of 128 x 128 on single CTAs: whichever has the busiest CTA finish first.  A pair's tile
-// is two of the others' work for each of its CTAs and fetches half as much per product.
-static bool gemm_pair_tiles(long long M, long long N, int batch, bool sym, int sms, int pairs) {
+// Tiles of 256 x 256 on CTA pairs, or of 128 x 128 on single CTAs: whichever has the busiest CTA finish first.  A K block of
+// `loads` tiles of 16 KB and `products` of them takes an SM 256 cycles a load (64 bytes a cycle from L2) or, for each product,
+// 512 cycles (128 x 256 of a pair's tile) or 256 (128 x 128): with one plane of each operand both kinds of tile take 512, and a
+// pair has done twice as much.
+static bool gemm_pair_tiles(long long M, long long N, int batch, bool sym, int a_planes, int b_planes, int sms, int pairs) {
   if (pairs < 1) return false;
   auto count = [&](int t) {
     const long long tm = (M + t - 1) / t, tn = (N + t - 1) / t;
     return (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
   };
-  const double pair = 2.0 * ((count(256) + pairs - 1) / pairs), single = 1.3 * ((count(128) + sms - 1) / sms);
+  const int loads = a_planes + b_planes, products = loads - 1;
+  const long long pair = std::max(256 * loads, 512 * products) * ((count(256) + pairs - 1) / pairs);
+  const long long single = std::max(256 * loads, 256 * products) * ((count(128) + sms - 1) / sms);
   return pair <= single;
 }
 

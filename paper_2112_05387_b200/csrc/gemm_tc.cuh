@@ -500,7 +500,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if constexpr (kPair) mbar_arrive_cluster(mapa_u32(smem_u32(&tail->tmem_empty[buf]), 0));
+          if constexpr (kPair) mbar_arrive_cluster_relaxed(mapa_u32(smem_u32(&tail->tmem_empty[buf]), 0));
           else mbar_arrive(&tail->tmem_empty[buf]);
         }
       };

@@ -7,6 +7,7 @@
 #include "linear_ce.cuh"
 #include "ops.h"
 #include "ortho.cuh"
+#include "ortho_small.cuh"
 
 namespace lp {
 
@@ -64,8 +65,78 @@ size_t ortho_scratch_bytes(int batch, int rows, int cols, bool split) {
   return c.off;
 }
 
-int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* launches) {
+// One launch for matrices whose X stays in the shared memory of a cluster (ortho_small.cuh): the smaller side is at most 128 and
+// the larger fits in 8 slices.  As many CTAs as the SMs hold at once, but slices of 32 columns at least.
+static const size_t kSmallMaxSmem = 224 * 1024;
+struct SmallShape { int S, ctas, slice; };
+static bool ortho_small_shape(int batch, int rows, int cols, bool split, int sms, SmallShape* out) {
+  const int s = std::min(rows, cols), l = std::max(rows, cols);
+  if (s > 128 || l > (1 << 20)) return false;
+  const int S = s <= 16 ? 16 : s <= 32 ? 32 : s <= 64 ? 64 : 128;
+  auto slice = [&](int c) { return ((l + c - 1) / c + 15) / 16 * 16; };
+  int c = 1;
+  while (c < 8 && (small_smem(S, slice(c), split) > kSmallMaxSmem || ((long long)batch * 2 * c <= sms && slice(2 * c) >= 32))) c *= 2;
+  if (small_smem(S, slice(c), split) > kSmallMaxSmem) return false;
+  *out = SmallShape{S, c, slice(c)};
+  return true;
+}
+template <bool kSplit, int S>
+static int start_small(const OrthoSmall& p, const SmallShape& sh, int batch, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(batch * sh.ctas));
+  cfg.blockDim = dim3(kSmallThreads);
+  cfg.dynamicSmemBytes = small_smem(S, sh.slice, kSplit);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = LP_PDL;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = sh.ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  LP_CUDA_OK(cudaLaunchKernelEx(&cfg, ortho_small_kernel<kSplit, S>, p));
+  return LP_OK;
+}
+template <int S>
+static int small_set_attributes() {
+  LP_CUDA_OK(cudaFuncSetAttribute(ortho_small_kernel<true, S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallMaxSmem));
+  LP_CUDA_OK(cudaFuncSetAttribute(ortho_small_kernel<false, S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallMaxSmem));
+  return LP_OK;
+}
+static int ortho_init_dev() {
   int rc = gemm_init_dev();
+  if (rc != LP_OK) return rc;
+  std::lock_guard<std::mutex> lock(g_devices_mutex);
+  Device& D = cur_dev();
+  if (D.ortho_attr) return LP_OK;
+  if ((rc = small_set_attributes<16>()) != LP_OK || (rc = small_set_attributes<32>()) != LP_OK ||
+      (rc = small_set_attributes<64>()) != LP_OK || (rc = small_set_attributes<128>()) != LP_OK)
+    return rc;
+  D.ortho_attr = true;
+  return LP_OK;
+}
+static int ortho_run_small(const OrthoProblem& q, const OrthoSource& src, const SmallShape& sh, int* err, cudaStream_t st) {
+  OrthoSmall p;
+  memset(&p, 0, sizeof(p));
+  p.src = src;
+  p.s = std::min(q.rows, q.cols);
+  p.l = std::max(q.rows, q.cols);
+  p.tall = q.rows > q.cols;
+  p.slice = sh.slice; p.ctas = sh.ctas; p.steps = q.steps;
+  p.a = q.coeffs[0]; p.b = q.coeffs[1]; p.c = q.coeffs[2]; p.eps = q.eps;
+  p.out = q.out; p.out_bf16 = q.out_bf16; p.update = q.update; p.keep = q.keep; p.step = q.step;
+  p.err = err;
+  switch (sh.S) {
+    case 16: return q.split ? start_small<true, 16>(p, sh, q.batch, st) : start_small<false, 16>(p, sh, q.batch, st);
+    case 32: return q.split ? start_small<true, 32>(p, sh, q.batch, st) : start_small<false, 32>(p, sh, q.batch, st);
+    case 64: return q.split ? start_small<true, 64>(p, sh, q.batch, st) : start_small<false, 64>(p, sh, q.batch, st);
+    default: return q.split ? start_small<true, 128>(p, sh, q.batch, st) : start_small<false, 128>(p, sh, q.batch, st);
+  }
+}
+
+int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* launches) {
+  int rc = ortho_init_dev();
   if (rc != LP_OK) return rc;
   const Device& D = cur_dev();
   Carve c{(uint8_t*)scratch};
@@ -83,6 +154,11 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   if (q.off) {
     src.use_off = 1;
     for (int b = 0; b < B; ++b) src.off[b] = q.off[b];
+  }
+  SmallShape small_shape;
+  if (ortho_small_shape(B, q.rows, q.cols, q.split, D.sm_count, &small_shape)) {
+    if (launches) *launches += 1;
+    return ortho_run_small(q, src, small_shape, s.err, st);
   }
   // bf16 gradients are exact in one plane; a momentum or an fp32 gradient is not
   int x_planes = (q.g_bf16 && !q.momentum && !q.split) ? 1 : 2;
@@ -103,8 +179,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   }
   if ((rc = encode_gemm_map(&m_a, GemmOperand{s.a, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
   if ((rc = encode_gemm_map(&m_b, GemmOperand{s.b, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
-  const bool pair_s = gemm_pair_tiles(small, small, B, true, D.sm_count, D.gemm_pairs);
-  const bool pair_x = gemm_pair_tiles(q.rows, q.cols, B, false, D.sm_count, D.gemm_pairs);
+  const bool pair_s = gemm_pair_tiles(small, small, B, true, planes, planes, D.sm_count, D.gemm_pairs);
 
   int cur = 0;
   for (int i = 0; i < q.steps; ++i) {
@@ -138,6 +213,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.b_planes = tall ? planes : x_planes;
     p.f = last ? 1.f / (first ? kScaleB : kScaleB * kScaleX) : (first ? kScaleX / kScaleB : 1.f / kScaleB);
     p.f_dev = s.alpha; p.f_pow = first ? 1 : 0;
+    const bool pair_x = gemm_pair_tiles(q.rows, q.cols, B, false, p.a_planes, p.b_planes, D.sm_count, D.gemm_pairs);
     const CUtensorMap& ma = tall ? m_xk[cur] : m_b;
     const CUtensorMap& mb = tall ? m_b : m_xm[cur];
     if (last) {
@@ -318,7 +394,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     const GemmOperand ox{(const uint16_t*)xm + (long long)r0 * ldx, D, rows, ldx, x_plane, planes, !s.f32};
     CUtensorMap m_xk, m_xm, m_pk, m_pm;
     if ((rc = encode_gemm_map(&m_xk, ox, false)) != LP_OK) return rc;
-    const bool pair = gemm_pair_tiles(rows, V, 1, false, Dv.sm_count, Dv.gemm_pairs);
+    const bool pair = gemm_pair_tiles(rows, V, 1, false, planes, planes, Dv.sm_count, Dv.gemm_pairs);
     const int part_cols = pair ? 128 : 64, parts = (V + (pair ? 255 : 127)) / (pair ? 256 : 128) * 2;
     tc::GemmParams p;
     memset(&p, 0, sizeof(p));
@@ -347,7 +423,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.a_planes = p.b_planes = planes;
       p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1;
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
-      const bool pr = gemm_pair_tiles(rows, D, 1, false, Dv.sm_count, Dv.gemm_pairs);
+      const bool pr = gemm_pair_tiles(rows, D, 1, false, planes, planes, Dv.sm_count, Dv.gemm_pairs);
       if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, pr, st)) != LP_OK) return rc;
     }
     if (dw) {
@@ -363,7 +439,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
         p.acc_first = r0 == 0;
         p.acc_last = r0 + rows == T;
       }
-      const bool pr = gemm_pair_tiles(V, D, 1, false, Dv.sm_count, Dv.gemm_pairs);
+      const bool pr = gemm_pair_tiles(V, D, 1, false, planes, planes, Dv.sm_count, Dv.gemm_pairs);
       if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, pr, st)) != LP_OK) return rc;
     }
   }

@@ -1,0 +1,314 @@
+// Orthogonalisation of small matrices in one launch: everything of a matrix stays in shared memory.
+//
+// With 15 dependent products of a few tiles each, a small matrix is bound by launches and by the way through global memory
+// and back (16 x 144: 85 us, its bytes take 10 ns).  Here a cluster of C CTAs holds X (smaller side S <= 128 padded to 16, 32, 64
+// or 128; the larger side in C slices) as fp16 high and low parts from the first pass to the last:
+//   partial = X_slice X_slice^T in every CTA;  cluster barrier;  every CTA adds up the C partials (distributed shared memory, in
+//   the same order: the same bits);  B = a I + b A + c A^2 in every CTA;  X_slice <- B X_slice in place.
+// Products are warp-level (mma.sync m16n8k16): the operands change hands between warps every few hundred cycles, and nothing is
+// large enough for the tensor memory's 128 rows to pay.  Sums of more than two K steps are added up in fp32 registers.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "ortho.cuh"
+
+namespace lp {
+
+constexpr int kSmallThreads = 256;
+constexpr int kSmallWarps = kSmallThreads / 32;
+
+struct OrthoSmall {
+  OrthoSource src;
+  int s, l;               // smaller and larger side
+  int tall;               // the matrix is l x s in memory
+  int slice, ctas;        // columns of a CTA's slice (a multiple of 16), CTAs of a cluster
+  int steps;
+  float a, b, c, eps;
+  void* out;
+  int out_bf16, update;
+  float keep, step;
+  int* err;
+};
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], const __half* p) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(tc::smem_u32(p)) : "memory");
+}
+__device__ __forceinline__ void ldsm2_trans(uint32_t (&r)[2], const __half* p) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];"
+               : "=r"(r[0]), "=r"(r[1]) : "r"(tc::smem_u32(p)) : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
+  double v;
+  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Shared memory: planes of X [2][S][slice + 8], of A [P][S][S + 8], then the partial sums [G][S][S] fp32 and, in the same place
+// later, the planes of B [P][S][S + 8].  P: 2 for fp32 results, else 1 (A and B are fp16).  G: K groups of the warps.
+__host__ __device__ constexpr int small_groups(int S) { return S == 16 ? 8 : (S == 32 ? 2 : 1); }
+__host__ __device__ inline size_t small_smem(int S, int slice, bool split) {
+  const size_t mat = (size_t)(split ? 2 : 1) * S * (S + 8) * 2, part = (size_t)small_groups(S) * S * S * 4;
+  return (size_t)2 * S * (slice + 8) * 2 + mat + (mat > part ? mat : part);
+}
+
+// Products of the 16 x 16 block (m0, n0) of P Q^T over K columns [k0, k1): planes of P and Q `pl` elements apart, rows `ld`.
+// kSplit: all parts but lo * lo.
+template <bool kSplit>
+__device__ __forceinline__ void small_block(float (&sum)[2][4], const __half* P, const __half* Q, int pl, int ld, int m0, int n0, int k0,
+                                            int k1, int lane) {
+  const __half* pa = P + (m0 + (lane & 15)) * ld + (lane >> 4) * 8;
+  // two 8-row tiles of Q: lanes 0-7 rows n0.., 8-15 the same 8 columns on, 16-31 rows n0 + 8..
+  const __half* qb = Q + (n0 + (lane & 7) + ((lane >> 4) << 3)) * ld + ((lane >> 3) & 1) * 8;
+#pragma unroll 1
+  for (int k = k0; k < k1; k += 32) {
+    float acc[2][4] = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int kk = k + 16 * h;
+      if (kk >= k1) break;
+      uint32_t ah[4], bh[4];
+      ldsm4(ah, pa + kk);
+      ldsm4(bh, qb + kk);
+      if constexpr (kSplit) {
+        uint32_t al[4], bl[4];
+        ldsm4(al, pa + pl + kk);
+        ldsm4(bl, qb + pl + kk);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          mma_f16(acc[t], ah, bl[2 * t], bl[2 * t + 1]);
+          mma_f16(acc[t], al, bh[2 * t], bh[2 * t + 1]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) mma_f16(acc[t], ah, bh[2 * t], bh[2 * t + 1]);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[t][i] += acc[t][i];
+  }
+}
+
+template <bool kSplit, int S>
+__global__ void __launch_bounds__(kSmallThreads, 1)
+ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
+  extern __shared__ __align__(16) uint8_t small_smem_raw[];
+  constexpr int P = kSplit ? 2 : 1, G = small_groups(S), LD = S + 8;
+  constexpr float kX = 4096.f, kA = 1024.f, kB = 1024.f;   // as in ortho_run
+  const int ldx = q.slice + 8, xpl = S * ldx;
+  __half* X = reinterpret_cast<__half*>(small_smem_raw);
+  __half* A = X + 2 * xpl;
+  float* part = reinterpret_cast<float*>(A + P * S * LD);
+  __half* B = reinterpret_cast<__half*>(part);
+  __shared__ double sums[kSmallWarps];
+  __shared__ double cta_sum;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_ctarank();
+  const int mat = blockIdx.x / q.ctas;
+  const long long base = q.src.use_off ? q.src.off[mat] : mat * q.src.elems;
+  const int j0 = (int)rank * q.slice, width = max(0, min(q.slice, q.l - j0));   // this CTA's columns
+
+  pdl_wait();
+  pdl_launch_dependents();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *q.err = 0;
+
+  // element e of the slice: row i of X, column j0 + j; contiguous in memory along j (wide) or i (tall)
+  const int n = q.s * width, inner = q.tall ? q.s : max(width, 1);
+  auto place = [&](int e, int& i, int& j, long long& at) {
+    const int hi = (int)((uint32_t)e / (uint32_t)inner), lo = e - hi * inner;
+    i = q.tall ? lo : hi;
+    j = q.tall ? hi : lo;
+    at = base + (q.tall ? (long long)(j0 + j) * q.s + i : (long long)i * q.l + j0 + j);
+  };
+  double sum = 0.0;
+#pragma unroll 4
+  for (int e = threadIdx.x; e < n; e += kSmallThreads) {
+    int i, j;
+    long long at;
+    place(e, i, j, at);
+    float u[1], m[1];
+    ortho_load<false>(q.src.g, q.src.g_bf16, at, u);
+    if (q.src.momentum) {
+      m[0] = fmaf(q.src.mu, q.src.momentum[at], u[0]);
+      q.src.momentum[at] = m[0];
+      ortho_direction(q.src, u, m);
+    }
+    sum += (double)u[0] * (double)u[0];
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) sums[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kSmallWarps; ++w) sum += sums[w];
+    cta_sum = sum;
+  }
+  // (rows and columns of the padding are zeros, and stay zeros)
+  for (int e = threadIdx.x; e < 2 * xpl / 8; e += kSmallThreads) reinterpret_cast<uint4*>(X)[e] = make_uint4(0u, 0u, 0u, 0u);
+  __syncthreads();
+  tc::cluster_sync_all();
+  sum = 0.0;
+  for (int r = 0; r < q.ctas; ++r) sum += ld_cluster_f64(tc::mapa_u32(tc::smem_u32(&cta_sum), r));
+  const float scale = (float)((double)kX / fmax(sqrt(sum), (double)q.eps));
+#pragma unroll 4
+  for (int e = threadIdx.x; e < n; e += kSmallThreads) {
+    int i, j;
+    long long at;
+    place(e, i, j, at);
+    float u[1], m[1];
+    ortho_load<false>(q.src.g, q.src.g_bf16, at, u);
+    if (q.src.momentum) {
+      m[0] = q.src.momentum[at];
+      ortho_direction(q.src, u, m);
+    }
+    __half hi, lo;
+    tc::split_half(u[0] * scale, hi, lo);
+    X[i * ldx + j] = hi;
+    X[xpl + i * ldx + j] = lo;
+  }
+  __syncthreads();
+
+  const int g = lane >> 2, t2 = 2 * (lane & 3);   // accumulator fragment: rows g, g + 8, columns t2, t2 + 1
+  constexpr int kBlocks = (S / 16) * (S / 16);
+  for (int step = 0; step < q.steps; ++step) {
+    const bool last = step + 1 == q.steps;
+    // partial sums of X X^T: 16 x 16 blocks over the warps, K in G groups where there are fewer blocks than warps
+    for (int w = warp; w < kBlocks * G; w += kSmallWarps) {
+      const int blk = w % kBlocks, grp = w / kBlocks;
+      const int m0 = blk / (S / 16) * 16, n0 = blk % (S / 16) * 16, ks = q.slice / 16;
+      float acc[2][4] = {};
+      small_block<kSplit>(acc, X, X, xpl, ldx, m0, n0, ks * grp / G * 16, ks * (grp + 1) / G * 16, lane);
+      float* o = part + grp * S * S + (m0 + g) * S + n0 + t2;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        *reinterpret_cast<float2*>(o + 8 * t) = make_float2(acc[t][0], acc[t][1]);
+        *reinterpret_cast<float2*>(o + 8 * S + 8 * t) = make_float2(acc[t][2], acc[t][3]);
+      }
+    }
+    __syncwarp();
+    tc::cluster_sync_all();
+    // four entries a thread; the CTAs' sums are all on their way before the first is added
+    for (int e = threadIdx.x * 4; e < S * S; e += kSmallThreads * 4) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < G; ++k) {
+        float4 x[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (r < q.ctas) x[r] = ld_cluster_f32x4(tc::mapa_u32(tc::smem_u32(part + k * S * S + e), r));
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (r < q.ctas) { v[0] += x[r].x; v[1] += x[r].y; v[2] += x[r].z; v[3] += x[r].w; }
+      }
+      __half hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tc::split_half(v[i] * (kA / (kX * kX)), hi[i], lo[i]);
+      __half* at = A + e / S * LD + e % S;
+      *reinterpret_cast<uint2*>(at) = make_uint2(tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]));
+      if constexpr (kSplit) *reinterpret_cast<uint2*>(at + S * LD) = make_uint2(tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]));
+    }
+    __syncthreads();
+    cluster_arrive();
+    // B, kept in registers until no CTA reads the partial sums any more
+    constexpr int kMine = (kBlocks + kSmallWarps - 1) / kSmallWarps;
+    float bv[kMine][2][4] = {};
+#pragma unroll
+    for (int u = 0; u < kMine; ++u) {
+      const int blk = warp + u * kSmallWarps;
+      if (blk >= kBlocks) break;
+      small_block<kSplit>(bv[u], A, A, S * LD, LD, blk / (S / 16) * 16, blk % (S / 16) * 16, 0, S, lane);
+    }
+    __syncwarp();
+    cluster_wait();
+#pragma unroll
+    for (int u = 0; u < kMine; ++u) {
+      const int blk = warp + u * kSmallWarps;
+      if (blk >= kBlocks) break;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = blk / (S / 16) * 16 + g + (i >> 1) * 8, c = blk % (S / 16) * 16 + 8 * t + t2 + (i & 1);
+          float av = __half2float(A[r * LD + c]);
+          if constexpr (kSplit) av += __half2float(A[S * LD + r * LD + c]);
+          const float v = fmaf(q.c * (kB / (kA * kA)), bv[u][t][i], q.b * (kB / kA) * av) + (r == c ? q.a * kB : 0.f);
+          __half hi, lo;
+          tc::split_half(v, hi, lo);
+          B[r * LD + c] = hi;
+          if constexpr (kSplit) B[S * LD + r * LD + c] = lo;
+        }
+    }
+    __syncthreads();
+    // X <- B X, 8 columns a warp: they are read into registers before any of them is written
+    for (int n0 = warp * 8; n0 < q.slice; n0 += kSmallWarps * 8) {
+      uint32_t xh[S / 16][2], xl[S / 16][2];
+#pragma unroll
+      for (int k = 0; k < S / 16; ++k) {
+        const __half* from = X + (16 * k + (lane & 15)) * ldx + n0;
+        ldsm2_trans(xh[k], from);
+        ldsm2_trans(xl[k], from + xpl);
+      }
+#pragma unroll 1
+      for (int m0 = 0; m0 < S; m0 += 16) {
+        float lo_acc[4] = {}, hi_acc[4] = {};
+#pragma unroll
+        for (int k = 0; k < S / 16; ++k) {
+          uint32_t bh[4];
+          const __half* from = B + (m0 + (lane & 15)) * LD + 16 * k + (lane >> 4) * 8;
+          ldsm4(bh, from);
+          mma_f16(lo_acc, bh, xl[k][0], xl[k][1]);
+          if constexpr (kSplit) {
+            uint32_t bl[4];
+            ldsm4(bl, from + S * LD);
+            mma_f16(lo_acc, bl, xh[k][0], xh[k][1]);
+          }
+          mma_f16(hi_acc, bh, xh[k][0], xh[k][1]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int i = m0 + g + 8 * h, j = n0 + t2;
+          const float v[2] = {(hi_acc[2 * h] + lo_acc[2 * h]) * (1.f / kB), (hi_acc[2 * h + 1] + lo_acc[2 * h + 1]) * (1.f / kB)};
+          if (!last) {
+            __half hi0, lo0, hi1, lo1;
+            tc::split_half(v[0], hi0, lo0);
+            tc::split_half(v[1], hi1, lo1);
+            *reinterpret_cast<uint32_t*>(X + i * ldx + j) = tc::pack_half2(hi0, hi1);
+            *reinterpret_cast<uint32_t*>(X + xpl + i * ldx + j) = tc::pack_half2(lo0, lo1);
+          } else if (i < q.s) {
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+              if (j + d >= width) continue;
+              const long long at = base + (q.tall ? (long long)(j0 + j + d) * q.s + i : (long long)i * q.l + j0 + j + d);
+              float x = v[d] * (1.f / kX);
+              if (q.out_bf16) {
+                bf16* o = (bf16*)q.out + at;
+                if (q.update) x = fmaf(q.step, x, q.keep * __bfloat162float(*o));
+                *o = __float2bfloat16_rn(x);
+              } else {
+                float* o = (float*)q.out + at;
+                if (q.update) x = fmaf(q.step, x, q.keep * *o);
+                *o = x;
+              }
+            }
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+  tc::cluster_sync_all();   // no CTA leaves while another may read its partial sums
+}
+
+}  // namespace lp

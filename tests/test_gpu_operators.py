@@ -179,7 +179,8 @@ def ortho_tol(dtype, steps=5):
 
 
 ORTHO_SIZES = [(1, 1, 1), (3, 1, 5), (3, 7, 1), (2, 16, 27), (5, 16, 144), (18, 64, 576), (2, 33, 31), (1, 127, 129), (1, 128, 128),
-               (2, 129, 257), (1, 257, 129), (3, 320, 64), (1, 640, 5760), (1, 2048, 512), (70, 24, 40), (1, 1000, 1003)]
+               (2, 129, 257), (1, 257, 129), (3, 320, 64), (1, 640, 5760), (1, 2048, 512), (70, 24, 40), (1, 1000, 1003),
+               (2, 128, 1152), (1, 5000, 7), (200, 64, 64), (1, 100, 40000), (3, 1152, 127), (1, 17, 33), (2, 3, 3000)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
