@@ -3,8 +3,8 @@
 // With 15 dependent products of a few tiles each, a small matrix is bound by launches and by the way through global memory
 // and back (16 x 144: 85 us, its bytes take 10 ns).  Here a cluster of C CTAs holds X (smaller side S <= 128 padded to 16, 32, 64
 // or 128; the larger side in C slices) as fp16 high and low parts from the first pass to the last:
-//   partial = X_slice X_slice^T in every CTA;  cluster barrier;  every CTA adds up the C partials (distributed shared memory, in
-//   the same order: the same bits);  B = a I + b A + c A^2 in every CTA;  X_slice <- B X_slice in place.
+//   partial = X_slice X_slice^T in every CTA;  cluster barrier;  every CTA adds up its share of the C partials and writes it to
+//   all (distributed shared memory);  cluster barrier;  B = a I + b A + c A^2 in every CTA;  X_slice <- B X_slice in place.
 // Products are warp-level (mma.sync m16n8k16): the operands change hands between warps every few hundred cycles, and nothing is
 // large enough for the tensor memory's 128 rows to pay.  Sums of more than two K steps are added up in fp32 registers.
 #pragma once
@@ -52,8 +52,9 @@ __device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
   asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void st_cluster_b32x2(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
 
 // Shared memory: planes of X [2][S][slice + 8], of A [P][S][S + 8], then the partial sums [G][S][S] fp32 and, in the same place
 // later, the planes of B [P][S][S + 8].  P: 2 for fp32 results, else 1 (A and B are fp16).  G: K groups of the warps.
@@ -199,8 +200,10 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
     }
     __syncwarp();
     tc::cluster_sync_all();
-    // four entries a thread; the CTAs' sums are all on their way before the first is added
-    for (int e = threadIdx.x * 4; e < S * S; e += kSmallThreads * 4) {
+    // each CTA adds up its share of the entries (the same order whatever the CTA), four a thread with all CTAs' sums on their way
+    // before the first is added, and writes them into every CTA's A: an entry crosses between SMs C times, not C^2
+    const int share = S * S / q.ctas;
+    for (int e = (int)rank * share + threadIdx.x * 4; e < (int)(rank + 1) * share; e += kSmallThreads * 4) {
       float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < G; ++k) {
@@ -215,13 +218,17 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
       __half hi[4], lo[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) tc::split_half(v[i] * (kA / (kX * kX)), hi[i], lo[i]);
-      __half* at = A + e / S * LD + e % S;
-      *reinterpret_cast<uint2*>(at) = make_uint2(tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]));
-      if constexpr (kSplit) *reinterpret_cast<uint2*>(at + S * LD) = make_uint2(tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]));
+      const uint32_t at = tc::smem_u32(A + e / S * LD + e % S);
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (r < q.ctas) {
+          const uint32_t to = tc::mapa_u32(at, r);
+          st_cluster_b32x2(to, tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]));
+          if constexpr (kSplit) st_cluster_b32x2(to + S * LD * 2, tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]));
+        }
     }
-    __syncthreads();
-    cluster_arrive();
-    // B, kept in registers until no CTA reads the partial sums any more
+    __syncwarp();
+    tc::cluster_sync_all();   // A is complete everywhere, and the partial sums have been read: B may take their place
     constexpr int kMine = (kBlocks + kSmallWarps - 1) / kSmallWarps;
     float bv[kMine][2][4] = {};
 #pragma unroll
@@ -230,8 +237,6 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
       if (blk >= kBlocks) break;
       small_block<kSplit>(bv[u], A, A, S * LD, LD, blk / (S / 16) * 16, blk % (S / 16) * 16, 0, S, lane);
     }
-    __syncwarp();
-    cluster_wait();
 #pragma unroll
     for (int u = 0; u < kMine; ++u) {
       const int blk = warp + u * kSmallWarps;
