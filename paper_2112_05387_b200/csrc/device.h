@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <mutex>
+#include <utility>
 
 #include "../../include/lp.h"
 #include "common.cuh"
@@ -77,10 +78,10 @@ static inline int grid_for(long long work_items, int threads, int sm_count, int 
   return (int)blocks;
 }
 
-// Launch with a cluster of two CTAs and programmatic stream serialisation allowed.
+// Launch with clusters of `ctas` CTAs and programmatic stream serialisation allowed.
 template <typename... KArgs, typename... Args>
-static inline cudaError_t launch_pdl_pair(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                                          Args&&... args) {
+static inline cudaError_t launch_pdl_cluster(int ctas, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
+                                             Args&&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -90,12 +91,16 @@ static inline cudaError_t launch_pdl_pair(void (*kernel)(KArgs...), dim3 grid, d
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = LP_PDL;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.x = (unsigned)ctas;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+template <typename... KArgs, typename... Args>
+static inline cudaError_t launch_pdl_pair(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+  return launch_pdl_cluster(2, kernel, grid, block, smem, st, std::forward<Args>(args)...);
 }
 
 }  // namespace lp

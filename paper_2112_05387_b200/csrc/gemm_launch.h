@@ -32,8 +32,10 @@ static int encode_gemm_map(CUtensorMap* m, const GemmOperand& o, bool mn) {
 
 template <int kEpi, int kMode>
 static int gemm_set_attributes() {
-  LP_CUDA_OK(cudaFuncSetAttribute(tc::gemm_tc_kernel<kEpi, true, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc::kGemmSmem));
-  LP_CUDA_OK(cudaFuncSetAttribute(tc::gemm_tc_kernel<kEpi, false, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc::kGemmSmem));
+  using namespace tc;
+  LP_CUDA_OK(cudaFuncSetAttribute(gemm_tc_kernel<kEpi, GEMM_SINGLE, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmSmem));
+  LP_CUDA_OK(cudaFuncSetAttribute(gemm_tc_kernel<kEpi, GEMM_PAIR, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmSmem));
+  LP_CUDA_OK(cudaFuncSetAttribute(gemm_tc_kernel<kEpi, GEMM_KSPLIT, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmSmem));
   return LP_OK;
 }
 // Kernel attributes, and how many CTA pairs the device holds at once (the grid is persistent: never more than that).
@@ -59,26 +61,30 @@ static int gemm_init_dev() {
   q.attrs = qa;
   q.numAttrs = 1;
   int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, tc::gemm_tc_kernel<tc::EPI_OUT, true, tc::GEMM_ONE>, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
+  if (cudaOccupancyMaxActiveClusters(&n, tc::gemm_tc_kernel<tc::EPI_OUT, tc::GEMM_PAIR, tc::GEMM_ONE>, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
   D.gemm_pairs = n;
   D.gemm_attr = true;
   return LP_OK;
 }
 
-// Tiles of 256 x 256 on CTA pairs, or of 128 x 128 on single CTAs: whichever has the busiest CTA finish first.  A K block of
-// `loads` tiles of 16 KB and `products` of them takes an SM 256 cycles a load (64 bytes a cycle from L2) or, for each product,
-// 512 cycles (128 x 256 of a pair's tile) or 256 (128 x 128): with one plane of each operand both kinds of tile take 512, and a
-// pair has done twice as much.
-static bool gemm_pair_tiles(long long M, long long N, int batch, bool sym, int a_planes, int b_planes, int sms, int pairs) {
-  if (pairs < 1) return false;
+// How a product is cut up: whichever way has its busiest CTA finish first.  A K block of `loads` tiles of 16 KB and `products` of
+// them takes an SM 256 cycles a load (64 bytes a cycle from L2) or, for each product, 512 cycles (128 x 256 of a pair's tile) or
+// 256 (128 x 128): with one plane of each operand a pair does twice as much in the time.  With fewer tiles than SMs a cluster of
+// four shares K, at the price of an exchange (about what eight K blocks take).
+static tc::GemmKind gemm_kind(long long M, long long N, long long K, int batch, bool sym, int a_planes, int b_planes) {
+  const Device& D = cur_dev();
   auto count = [&](int t) {
     const long long tm = (M + t - 1) / t, tn = (N + t - 1) / t;
     return (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
   };
   const int loads = a_planes + b_planes, products = loads - 1;
-  const long long pair = std::max(256 * loads, 512 * products) * ((count(256) + pairs - 1) / pairs);
-  const long long single = std::max(256 * loads, 256 * products) * ((count(128) + sms - 1) / sms);
-  return pair <= single;
+  const long long kb = (K + 63) / 64, c_pair = std::max(256 * loads, 512 * products), c_single = std::max(256 * loads, 256 * products);
+  const int pairs = std::max(D.gemm_pairs, 1), quads = D.sm_count / 4;
+  const long long pair = D.gemm_pairs < 1 ? (1LL << 62) : kb * c_pair * ((count(256) + pairs - 1) / pairs);
+  const long long single = kb * c_single * ((count(128) + D.sm_count - 1) / D.sm_count);
+  const long long split = kb < 4 ? (1LL << 62) : ((kb + 3) / 4 + 8) * c_single * ((count(128) + quads - 1) / quads);
+  if (split < pair && split < single) return tc::GEMM_KSPLIT;
+  return pair <= single ? tc::GEMM_PAIR : tc::GEMM_SINGLE;
 }
 
 // K blocks of 64 that the tensor core adds up before its accumulator is emptied into registers where fp32 results are wanted.
@@ -88,17 +94,22 @@ static bool gemm_pair_tiles(long long M, long long N, int batch, bool sym, int a
 constexpr int kGemmRound = LP_GEMM_ROUND;
 
 template <int kEpi, int kMode>
-static cudaError_t start_gemm(const tc::GemmParams& p, const CUtensorMap& ma, const CUtensorMap& mb, bool pair, cudaStream_t st) {
+static cudaError_t start_gemm(const tc::GemmParams& p, const CUtensorMap& ma, const CUtensorMap& mb, tc::GemmKind kind, cudaStream_t st) {
+  using namespace tc;
   const Device& D = cur_dev();
-  const dim3 block(tc::kGemmThreads);
-  return pair ? launch_pdl_pair(tc::gemm_tc_kernel<kEpi, true, kMode>, dim3(2 * std::min(p.total_tiles, D.gemm_pairs)), block, tc::kGemmSmem, st,
-                                ma, mb, p)
-              : launch_pdl(tc::gemm_tc_kernel<kEpi, false, kMode>, dim3(std::min(p.total_tiles, D.sm_count)), block, tc::kGemmSmem, st, ma, mb, p);
+  const dim3 block(kGemmThreads);
+  if (kind == GEMM_PAIR)
+    return launch_pdl_cluster(2, gemm_tc_kernel<kEpi, GEMM_PAIR, kMode>, dim3(2 * std::min(p.total_tiles, D.gemm_pairs)), block, kGemmSmem, st,
+                              ma, mb, p);
+  if (kind == GEMM_KSPLIT)
+    return launch_pdl_cluster(4, gemm_tc_kernel<kEpi, GEMM_KSPLIT, kMode>, dim3(4 * p.total_tiles), block, kGemmSmem, st, ma, mb, p);
+  return launch_pdl(gemm_tc_kernel<kEpi, GEMM_SINGLE, kMode>, dim3(std::min(p.total_tiles, D.sm_count)), block, kGemmSmem, st, ma, mb, p);
 }
 // Launches the product.  Sizes, planes and the epilogue's fields of `p` are the caller's; the rest is filled in here.
 template <int kEpi>
 static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bool a_mn, const CUtensorMap& mb, bool b_mn, bool bf16,
-                       bool pair, cudaStream_t st) {
+                       tc::GemmKind kind, cudaStream_t st) {
+  const bool pair = kind == tc::GEMM_PAIR;
   const int tile = pair ? 256 : 128;
   p.tiles_m = (p.M + tile - 1) / tile;
   p.tiles_n = (p.N + tile - 1) / tile;
@@ -120,9 +131,9 @@ static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bo
     p.out_vec = vec;
   }
   cudaError_t e;
-  if (p.a_planes == 1 && p.b_planes == 1) e = start_gemm<kEpi, tc::GEMM_ONE>(p, ma, mb, pair, st);
-  else if (p.a_planes == 2 && p.b_planes == 2) e = start_gemm<kEpi, tc::GEMM_SPLIT>(p, ma, mb, pair, st);
-  else if constexpr (kEpi != tc::EPI_CE) e = start_gemm<kEpi, tc::GEMM_LOW>(p, ma, mb, pair, st);
+  if (p.a_planes == 1 && p.b_planes == 1) e = start_gemm<kEpi, tc::GEMM_ONE>(p, ma, mb, kind, st);
+  else if (p.a_planes == 2 && p.b_planes == 2) e = start_gemm<kEpi, tc::GEMM_SPLIT>(p, ma, mb, kind, st);
+  else if constexpr (kEpi != tc::EPI_CE) e = start_gemm<kEpi, tc::GEMM_LOW>(p, ma, mb, kind, st);
   else return LP_ERR_UNSUPPORTED;
   LP_CUDA_OK(e);
   return LP_OK;

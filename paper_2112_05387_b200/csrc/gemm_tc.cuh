@@ -83,7 +83,7 @@ struct GemmParams {
   const void* bias;               // [N] in the operands' type or null
   int bias_bf16;
   const int32_t* labels;          // [M]
-  float2* stats;                  // [column half][M]: maximum, sum of exponentials
+  float2* stats;                  // [part of the columns][M]: maximum, sum of exponentials
   long long stats_ld;
   float* target;                  // [M]: the label's logit
   // (h_out, h_ld, h_plane: exponentials relative to the half's maximum, times 2^14; null: not kept)
@@ -328,8 +328,14 @@ enum GemmMode {
   GEMM_SPLIT = 2,    // both parts of both, in rounds
 };
 
-// kPair: tiles of 256 x 256 on CTA pairs, else 128 x 128 on single CTAs.
-template <int kEpi, bool kPair, int kMode>
+// How a tile is computed.
+enum GemmKind {
+  GEMM_SINGLE = 0,   // 128 x 128 by one CTA
+  GEMM_PAIR = 1,     // 256 x 256 by a CTA pair
+  GEMM_KSPLIT = 2,   // 128 x 128 by a cluster of four CTAs, a quarter of K each; one tile a cluster
+};
+
+template <int kEpi, int kKind, int kMode>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ GemmParams p) {
   extern __shared__ uint8_t smem_raw[];
@@ -338,12 +344,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   GemmTail* tail = reinterpret_cast<GemmTail*>(scratch_all + kGemmEpiWarps * kGemmScratchFloats);
   volatile int* abort_flag = &tail->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kCtas = kPair ? 2 : 1;
+  constexpr bool kPair = kKind == GEMM_PAIR, kKSplit = kKind == GEMM_KSPLIT;
+  constexpr int kCtas = kPair ? 2 : 1, kCluster = kKSplit ? 4 : kCtas;
   constexpr int kTileM = 128 * kCtas, kTileN = 128 * kCtas;
   constexpr uint32_t kAccCols = kTileN, kTmem = 2 * kAccCols;
-  const uint32_t rank = kPair ? cluster_ctarank() : 0;
+  const uint32_t crank = kCluster > 1 ? cluster_ctarank() : 0;
+  const uint32_t rank = kPair ? crank : 0;      // of the CTAs that share a tile's rows
   const bool leader = rank == 0;
-  const int unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
+  const int unit = blockIdx.x / kCluster, units = gridDim.x / kCluster;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kGemmStages; ++s) {
@@ -370,12 +378,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   }
   tc_fence_before();
   __syncthreads();
-  if constexpr (kPair) cluster_sync_all();   // both CTAs' barriers exist before anything signals them from the other side
+  if constexpr (kCluster > 1) cluster_sync_all();   // both CTAs' barriers exist before anything signals them from the other side
   tc_fence_after();
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t tmem_base = tail->tmem_base;
-  const int steps = p.kblocks;
+  // (a quarter of K: at least one K block, see gemm_kind)
+  const int k_first = kKSplit ? p.kblocks * (int)crank / 4 : 0;
+  const int steps = kKSplit ? p.kblocks * (int)(crank + 1) / 4 - k_first : p.kblocks;
   constexpr bool kRounds = kMode == GEMM_SPLIT;
   const int round_len = kRounds ? p.round_len : steps;
   constexpr uint32_t kTiles = 2 + kMode, kStages = 12 / kTiles, kStageBytes = kTiles * kGemmTileBytes;
@@ -393,7 +403,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         if (!mbar_wait_warp(&tail->empty[s], ph ^ 1, abort_flag)) { failed = true; break; }
         if (elect_one()) {
           uint8_t* dst = smem + s * kStageBytes;
-          const int k0 = i * 64;
+          const int k0 = (k_first + i) * 64;
           uint64_t* full = &tail->full[s];
           const uint32_t fb = kPair ? mapa_u32(smem_u32(full), 0) : 0;
           if (leader) mbar_expect_tx(full, kCtas * kStageBytes);
@@ -486,7 +496,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       int b, tm, tn;
       gemm_tile(p, t, b, tm, tn);
       const int row0 = tm * kTileM + (int)rank * 128 + q * 32, row = row0 + lane;
-      const int col0 = tn * kTileN + half * (kTileN / 2);
+      int col0 = tn * kTileN + half * (kTileN / 2);
       const float f = gemm_scale(p, b);
       float acc[kRounds ? kGroups : 1][32];
       if constexpr (kRounds) {
@@ -522,15 +532,50 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         buf ^= 1;
         if (!buf) bph ^= 1;
       }
-      if (failed) break;
+      if (failed && !kKSplit) break;
+      int groups = kGroups;
       if constexpr (kRounds) {   // the sum goes back to where the accumulator was: what follows reads it group by group
+        if (!failed) {
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) tmem_st32(taddr + g * 32, acc[g]);
+          for (int g = 0; g < kGroups; ++g) tmem_st32(taddr + g * 32, acc[g]);
+        }
+      }
+      if constexpr (kKSplit) {
+        // Each CTA of the cluster finishes one group of 32 columns: the other three send it their sums, into its ring (its own
+        // products have read it: the first barrier).  The warps that have the CTA's group add them up and go on with it.
+        float* ring = reinterpret_cast<float*>(smem);
+        cluster_sync_all();
+        if (!failed) {
+#pragma unroll 1
+          for (int g = 0; g < kGroups; ++g) {
+            const uint32_t to = half * kGroups + g;
+            if (to == crank) continue;
+            float v[32];
+            tmem_ld32(taddr + g * 32, v);
+            const uint32_t at = mapa_u32(smem_u32(ring + (crank * 32) * 128 + q * 32 + lane), to);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) st_cluster_f32(at + j * 512, v[j]);
+          }
+        }
+        cluster_sync_all();
+        const int mine = (int)crank - half * kGroups;
+        if (failed || mine < 0 || mine >= kGroups) break;
+        taddr += mine * 32;
+        float v[32];
+        tmem_ld32(taddr, v);
+        for (int r = 0; r < 4; ++r)
+          if (r != (int)crank) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += ring[(r * 32 + j) * 128 + q * 32 + lane];
+          }
+        tmem_st32(taddr, v);
+        col0 = tn * kTileN + (int)crank * 32;
+        groups = 1;
       }
       if constexpr (kEpi == EPI_CE) {
         float top = -INFINITY;
 #pragma unroll 1
-        for (int g = 0; g < kGroups; ++g) {
+        for (int g = 0; g < groups; ++g) {
           float v[32];
           tmem_ld32(taddr + g * 32, v);
           ce_logits(p, col0 + g * 32, f, lane, v);
@@ -541,11 +586,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const int label = row < p.M ? p.labels[row] : -1;
         float sum = 0.f;
 #pragma unroll 1
-        for (int g = 0; g < kGroups; ++g) {
+        for (int g = 0; g < groups; ++g) {
           const int col = col0 + g * 32;
           float v[32];
           tmem_ld32(taddr + g * 32, v);
-          if (g + 1 == kGroups) release();
+          if (g + 1 == groups) release();
           ce_logits(p, col, f, lane, v);
           if (label >= col && label < col + 32) {
 #pragma unroll
@@ -559,15 +604,15 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
           if (p.h_out && col < p.N) epi_h16(p, 0, row, col, false, v);
         }
-        if (row < p.M) p.stats[(long long)(tn * 2 + half) * p.stats_ld + row] = make_float2(ref, sum * 6.103515625e-5f);
+        if (row < p.M) p.stats[(long long)(kKSplit ? tn * 4 + (int)crank : tn * 2 + half) * p.stats_ld + row] = make_float2(ref, sum * 6.103515625e-5f);
       } else {
         const bool mirror = p.sym && tm != tn;
 #pragma unroll 1
-        for (int g = 0; g < kGroups; ++g) {
+        for (int g = 0; g < groups; ++g) {
           const int col = col0 + g * 32;
           float v[32];
           tmem_ld32(taddr + g * 32, v);
-          if (g + 1 == kGroups) release();
+          if (g + 1 == groups) release();
           if (col >= p.N) continue;
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] *= f;
@@ -581,6 +626,13 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     }
   }
 
+  if constexpr (kKSplit) {
+    if (warp < 2) {   // the two barriers of the exchange are for every thread
+      __syncwarp();
+      cluster_sync_all();
+      cluster_sync_all();
+    }
+  }
   if (failed) {
     *abort_flag = 1;
     atomicExch(p.err, 1);
@@ -595,7 +647,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll 1
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
   }
-  if constexpr (kPair) cluster_sync_all();   // neither CTA leaves while the other may still signal it
+  if constexpr (kCluster > 1) cluster_sync_all();   // no CTA leaves while another may still signal it or write its ring
   if (warp == 2) {
     tc_fence_after();
     if constexpr (kPair) tmem2_dealloc(tmem_base, kTmem);

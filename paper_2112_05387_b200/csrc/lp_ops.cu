@@ -82,20 +82,8 @@ static bool ortho_small_shape(int batch, int rows, int cols, bool split, int sms
 }
 template <bool kSplit, int S>
 static int start_small(const OrthoSmall& p, const SmallShape& sh, int batch, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(batch * sh.ctas));
-  cfg.blockDim = dim3(kSmallThreads);
-  cfg.dynamicSmemBytes = small_smem(S, sh.slice, kSplit);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = LP_PDL;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = sh.ctas;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  LP_CUDA_OK(cudaLaunchKernelEx(&cfg, ortho_small_kernel<kSplit, S>, p));
+  LP_CUDA_OK(launch_pdl_cluster(sh.ctas, ortho_small_kernel<kSplit, S>, dim3((unsigned)(batch * sh.ctas)), dim3(kSmallThreads),
+                                small_smem(S, sh.slice, kSplit), st, p));
   return LP_OK;
 }
 template <int S>
@@ -179,7 +167,8 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   }
   if ((rc = encode_gemm_map(&m_a, GemmOperand{s.a, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
   if ((rc = encode_gemm_map(&m_b, GemmOperand{s.b, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
-  const bool pair_s = gemm_pair_tiles(small, small, B, true, planes, planes, D.sm_count, D.gemm_pairs);
+  const tc::GemmKind kind_g = gemm_kind(small, small, tall ? q.rows : q.cols, B, true, planes, planes),
+                     kind_a = gemm_kind(small, small, small, B, true, planes, planes);
 
   int cur = 0;
   for (int i = 0; i < q.steps; ++i) {
@@ -192,8 +181,8 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.f = first ? kScaleA : kScaleA / (kScaleX * kScaleX);
     p.f_dev = s.alpha; p.f_pow = first ? 2 : 0;
     p.h_out = s.a; p.h_ld = s.ld_s; p.h_batch = s_mat; p.h_plane = q.split ? s_plane : 0;
-    if (tall) rc = launch_gemm<tc::EPI_H16>(p, q.rows, m_xm[cur], true, m_xm[cur], true, false, pair_s, st);
-    else rc = launch_gemm<tc::EPI_H16>(p, q.cols, m_xk[cur], false, m_xk[cur], false, false, pair_s, st);
+    if (tall) rc = launch_gemm<tc::EPI_H16>(p, q.rows, m_xm[cur], true, m_xm[cur], true, false, kind_g, st);
+    else rc = launch_gemm<tc::EPI_H16>(p, q.cols, m_xk[cur], false, m_xk[cur], false, false, kind_g, st);
     if (rc != LP_OK) return rc;
     // B = a I + b A + c A^2
     memset(&p, 0, sizeof(p));
@@ -202,7 +191,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.f = q.coeffs[2] * (kScaleB / (kScaleA * kScaleA));
     p.h_out = s.b; p.h_ld = s.ld_s; p.h_batch = s_mat; p.h_plane = q.split ? s_plane : 0;
     p.aux = s.a; p.aux_f = q.coeffs[1] * (kScaleB / kScaleA); p.diag = q.coeffs[0] * kScaleB;
-    rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, pair_s, st);
+    rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, kind_a, st);
     if (rc != LP_OK) return rc;
     // X <- B X (X B).  An error in X grows by up to a in each later step, so its low part is kept while three or more
     // products follow (relative error of the result, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3 with the
@@ -213,7 +202,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.b_planes = tall ? planes : x_planes;
     p.f = last ? 1.f / (first ? kScaleB : kScaleB * kScaleX) : (first ? kScaleX / kScaleB : 1.f / kScaleB);
     p.f_dev = s.alpha; p.f_pow = first ? 1 : 0;
-    const bool pair_x = gemm_pair_tiles(q.rows, q.cols, B, false, p.a_planes, p.b_planes, D.sm_count, D.gemm_pairs);
+    const tc::GemmKind kind_x = gemm_kind(q.rows, q.cols, small, B, false, p.a_planes, p.b_planes);
     const CUtensorMap& ma = tall ? m_xk[cur] : m_b;
     const CUtensorMap& mb = tall ? m_b : m_xm[cur];
     if (last) {
@@ -223,12 +212,12 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
         p.use_off = 1;
         for (int b = 0; b < B; ++b) p.off[b] = q.off[b];
       }
-      rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, pair_x, st);
+      rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, kind_x, st);
     } else {
       x_planes = (q.split || i + 3 < q.steps) ? 2 : 1;
       cur ^= 1;
       p.h_out = s.x[cur]; p.h_ld = s.ld; p.h_batch = x_mat; p.h_plane = x_planes == 2 ? x_plane : 0;
-      rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, pair_x, st);
+      rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, kind_x, st);
     }
     if (rc != LP_OK) return rc;
     n += 3;
@@ -272,8 +261,8 @@ static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) 
   const int planes = s.f32 ? 2 : 1;
   s.ld_v = row_stride(V);
   s.ld_d = (D + 7) / 8 * 8;
-  // (the loss alone keeps 16 bytes for each row and 128 classes)
-  const size_t row_bytes = grads ? (size_t)s.ld_v * 2 * planes : (size_t)((V + 127) / 128) * 16;
+  // (the loss alone keeps up to 32 bytes for each row and 128 classes)
+  const size_t row_bytes = grads ? (size_t)s.ld_v * 2 * planes : (size_t)((V + 127) / 128) * 32;
   const bool whole = grads && !s.f32 && (size_t)T * row_bytes <= (size_t)V * D * 4;
   const long long fit = whole ? T : (long long)(kCePieceBytes / row_bytes) / 256 * 256;
   s.rows = (int)std::min<long long>(T, std::min(std::max(256LL, fit), 1LL << 18));
@@ -286,7 +275,7 @@ static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) 
   s.target = c.take<float>(T);
   s.lse = c.take<float>(T);
   s.row_loss = c.take<float>(T);
-  s.stats = c.take<float2>((size_t)2 * ((V + 127) / 128) * s.rows);
+  s.stats = c.take<float2>((size_t)4 * ((V + 127) / 128) * s.rows);
   const bool pack_x = s.pack_w || grads;
   s.x = pack_x ? c.take<__half>((size_t)planes * T * s.ld_d) : nullptr;
   s.w = s.pack_w ? c.take<__half>((size_t)planes * V * s.ld_d) : nullptr;
@@ -394,8 +383,9 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     const GemmOperand ox{(const uint16_t*)xm + (long long)r0 * ldx, D, rows, ldx, x_plane, planes, !s.f32};
     CUtensorMap m_xk, m_xm, m_pk, m_pm;
     if ((rc = encode_gemm_map(&m_xk, ox, false)) != LP_OK) return rc;
-    const bool pair = gemm_pair_tiles(rows, V, 1, false, planes, planes, Dv.sm_count, Dv.gemm_pairs);
-    const int part_cols = pair ? 128 : 64, parts = (V + (pair ? 255 : 127)) / (pair ? 256 : 128) * 2;
+    const tc::GemmKind kind = gemm_kind(rows, V, D, 1, false, planes, planes);
+    const int part_cols = kind == tc::GEMM_PAIR ? 128 : kind == tc::GEMM_SINGLE ? 64 : 32;
+    const int parts = (V + part_cols - 1) / part_cols;
     tc::GemmParams p;
     memset(&p, 0, sizeof(p));
     p.M = rows; p.N = V; p.batch = 1; p.err = &s.hdr->err;
@@ -404,7 +394,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     p.bias = bias; p.bias_bf16 = is_bf16; p.labels = labels + r0;
     p.stats = s.stats; p.stats_ld = s.rows; p.target = s.target + r0;
     p.h_out = s.p; p.h_ld = s.ld_v; p.h_plane = s.f32 ? p_plane : 0;
-    if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, pair, st)) != LP_OK) return rc;
+    if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, kind, st)) != LP_OK) return rc;
     LP_CUDA_OK(launch_pdl(ce_rows_kernel, dim3((rows + 7) / 8), dim3(kCeThreads), 0, st, (const float2*)s.stats, (long long)s.rows, parts,
                           rows, V, labels + r0, (const float*)(s.target + r0), s.lse + r0, rl + r0));
     if (!grads) continue;
@@ -423,8 +413,8 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.a_planes = p.b_planes = planes;
       p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1;
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
-      const bool pr = gemm_pair_tiles(rows, D, 1, false, planes, planes, Dv.sm_count, Dv.gemm_pairs);
-      if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, pr, st)) != LP_OK) return rc;
+      const tc::GemmKind kd = gemm_kind(rows, D, V, 1, false, planes, planes);
+      if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, kd, st)) != LP_OK) return rc;
     }
     if (dw) {
       if ((rc = encode_gemm_map(&m_pm, op, true)) != LP_OK) return rc;
@@ -439,8 +429,8 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
         p.acc_first = r0 == 0;
         p.acc_last = r0 + rows == T;
       }
-      const bool pr = gemm_pair_tiles(V, D, 1, false, planes, planes, Dv.sm_count, Dv.gemm_pairs);
-      if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, pr, st)) != LP_OK) return rc;
+      const tc::GemmKind kd = gemm_kind(V, D, rows, 1, false, planes, planes);
+      if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, kd, st)) != LP_OK) return rc;
     }
   }
   if (dbias)
