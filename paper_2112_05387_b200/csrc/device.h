@@ -35,9 +35,10 @@ struct Device {
   EncodeTiledFn encode = nullptr;
   // kernel attributes are per device: set on the first launch of each kernel family on that device
   bool conv_attr = false, wgrad_attr = false, wgrad_halo_attr = false, conv2_attr = false, f32_attr = false, thin_attr = false,
-       gemm_attr = false, ortho_attr = false;
+       gemm_attr = false, ortho_attr = false, ce_attr = false;
   int max_pairs = 0;   // CTA pairs of conv_tc2_kernel that can be resident at once (0: not usable)
   int gemm_pairs = 0;  // the same for gemm_tc_kernel
+  int gemm_clusters[5] = {0};  // and its clusters of 2 to 4 CTAs that share K
   int init() {
     if (ready) return LP_OK;
     int dev = 0;

@@ -51,40 +51,57 @@ static int gemm_init_dev() {
       (rc = gemm_set_attributes<EPI_OUT, GEMM_LOW>()) != LP_OK || (rc = gemm_set_attributes<EPI_OUT, GEMM_SPLIT>()) != LP_OK ||
       (rc = gemm_set_attributes<EPI_CE, GEMM_ONE>()) != LP_OK || (rc = gemm_set_attributes<EPI_CE, GEMM_SPLIT>()) != LP_OK)
     return rc;
-  cudaLaunchConfig_t q = {};
-  q.gridDim = dim3(2 * D.sm_count);
-  q.blockDim = dim3(tc::kGemmThreads);
-  q.dynamicSmemBytes = tc::kGemmSmem;
-  cudaLaunchAttribute qa[1];
-  qa[0].id = cudaLaunchAttributeClusterDimension;
-  qa[0].val.clusterDim.x = 2; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
-  q.attrs = qa;
-  q.numAttrs = 1;
-  int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, tc::gemm_tc_kernel<tc::EPI_OUT, tc::GEMM_PAIR, tc::GEMM_ONE>, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
-  D.gemm_pairs = n;
+  auto clusters = [&](int ctas, auto kernel) {
+    cudaLaunchConfig_t q = {};
+    q.gridDim = dim3(ctas * D.sm_count);
+    q.blockDim = dim3(kGemmThreads);
+    q.dynamicSmemBytes = kGemmSmem;
+    cudaLaunchAttribute qa[1];
+    qa[0].id = cudaLaunchAttributeClusterDimension;
+    qa[0].val.clusterDim.x = ctas; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
+    q.attrs = qa;
+    q.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
+    return n;
+  };
+  D.gemm_pairs = clusters(2, gemm_tc_kernel<EPI_OUT, GEMM_PAIR, GEMM_ONE>);
+  for (int c = 2; c <= 4; ++c) D.gemm_clusters[c] = clusters(c, gemm_tc_kernel<EPI_OUT, GEMM_KSPLIT, GEMM_ONE>);
   D.gemm_attr = true;
   return LP_OK;
 }
 
-// How a product is cut up: whichever way has its busiest CTA finish first.  A K block of `loads` tiles of 16 KB and `products` of
-// them takes an SM 256 cycles a load (64 bytes a cycle from L2) or, for each product, 512 cycles (128 x 256 of a pair's tile) or
-// 256 (128 x 128): with one plane of each operand a pair does twice as much in the time.  With fewer tiles than SMs a cluster of
-// four shares K, at the price of an exchange (about what eight K blocks take).
-static tc::GemmKind gemm_kind(long long M, long long N, long long K, int batch, bool sym, int a_planes, int b_planes) {
+// How a product is cut up.
+struct GemmCut {
+  tc::GemmKind kind;
+  int ctas;          // of a cluster
+};
+// Whichever way has its busiest CTA finish first.  A K block of `loads` tiles of 16 KB and `products` of them takes an SM 256
+// cycles a load (64 bytes a cycle from L2) or, for each product, 512 cycles (128 x 256 of a pair's tile; 690 with one plane of
+// each operand, measured: 0.47 us with 42 pairs at work) or 256 (128 x 128).  With few tiles a cluster shares K, at the price of
+// an exchange (two K blocks or so); of four CTAs at most (16 K blocks over eight: 21 us, over four: 13).
+static GemmCut gemm_cut(long long M, long long N, long long K, int batch, bool sym, int a_planes, int b_planes) {
   const Device& D = cur_dev();
   auto count = [&](int t) {
     const long long tm = (M + t - 1) / t, tn = (N + t - 1) / t;
     return (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
   };
+  auto waves = [](long long n, int at_once) { return (n + at_once - 1) / at_once; };
   const int loads = a_planes + b_planes, products = loads - 1;
-  const long long kb = (K + 63) / 64, c_pair = std::max(256 * loads, 512 * products), c_single = std::max(256 * loads, 256 * products);
-  const int pairs = std::max(D.gemm_pairs, 1), quads = D.sm_count / 4;
-  const long long pair = D.gemm_pairs < 1 ? (1LL << 62) : kb * c_pair * ((count(256) + pairs - 1) / pairs);
-  const long long single = kb * c_single * ((count(128) + D.sm_count - 1) / D.sm_count);
-  const long long split = kb < 4 ? (1LL << 62) : ((kb + 3) / 4 + 8) * c_single * ((count(128) + quads - 1) / quads);
-  if (split < pair && split < single) return tc::GEMM_KSPLIT;
-  return pair <= single ? tc::GEMM_PAIR : tc::GEMM_SINGLE;
+  const long long kb = (K + 63) / 64, c_pair = std::max(256 * loads, products == 1 ? 690 : 512 * products),
+                  c_single = std::max(256 * loads, 256 * products);
+  GemmCut best{tc::GEMM_SINGLE, 1};
+  long long time = (kb + 2) * c_single * waves(count(128), D.sm_count);
+  if (D.gemm_pairs > 0) {
+    const long long t = (kb + 2) * c_pair * waves(count(256), D.gemm_pairs);
+    if (t <= time) { best = GemmCut{tc::GEMM_PAIR, 2}; time = t; }
+  }
+  for (int c = 2; c <= 4 && c <= kb; ++c) {
+    if (D.gemm_clusters[c] < 1) continue;
+    const long long t = ((kb + c - 1) / c + 4) * c_single * waves(count(128), D.gemm_clusters[c]);
+    if (t < time) { best = GemmCut{tc::GEMM_KSPLIT, c}; time = t; }
+  }
+  return best;
 }
 
 // K blocks of 64 that the tensor core adds up before its accumulator is emptied into registers where fp32 results are wanted.
@@ -94,22 +111,22 @@ static tc::GemmKind gemm_kind(long long M, long long N, long long K, int batch, 
 constexpr int kGemmRound = LP_GEMM_ROUND;
 
 template <int kEpi, int kMode>
-static cudaError_t start_gemm(const tc::GemmParams& p, const CUtensorMap& ma, const CUtensorMap& mb, tc::GemmKind kind, cudaStream_t st) {
+static cudaError_t start_gemm(const tc::GemmParams& p, const CUtensorMap& ma, const CUtensorMap& mb, const GemmCut& cut, cudaStream_t st) {
   using namespace tc;
   const Device& D = cur_dev();
   const dim3 block(kGemmThreads);
-  if (kind == GEMM_PAIR)
+  if (cut.kind == GEMM_PAIR)
     return launch_pdl_cluster(2, gemm_tc_kernel<kEpi, GEMM_PAIR, kMode>, dim3(2 * std::min(p.total_tiles, D.gemm_pairs)), block, kGemmSmem, st,
                               ma, mb, p);
-  if (kind == GEMM_KSPLIT)
-    return launch_pdl_cluster(4, gemm_tc_kernel<kEpi, GEMM_KSPLIT, kMode>, dim3(4 * p.total_tiles), block, kGemmSmem, st, ma, mb, p);
+  if (cut.kind == GEMM_KSPLIT)
+    return launch_pdl_cluster(cut.ctas, gemm_tc_kernel<kEpi, GEMM_KSPLIT, kMode>, dim3(cut.ctas * p.total_tiles), block, kGemmSmem, st, ma, mb, p);
   return launch_pdl(gemm_tc_kernel<kEpi, GEMM_SINGLE, kMode>, dim3(std::min(p.total_tiles, D.sm_count)), block, kGemmSmem, st, ma, mb, p);
 }
 // Launches the product.  Sizes, planes and the epilogue's fields of `p` are the caller's; the rest is filled in here.
 template <int kEpi>
 static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bool a_mn, const CUtensorMap& mb, bool b_mn, bool bf16,
-                       tc::GemmKind kind, cudaStream_t st) {
-  const bool pair = kind == tc::GEMM_PAIR;
+                       const GemmCut& cut, cudaStream_t st) {
+  const bool pair = cut.kind == tc::GEMM_PAIR;
   const int tile = pair ? 256 : 128;
   p.tiles_m = (p.M + tile - 1) / tile;
   p.tiles_n = (p.N + tile - 1) / tile;
@@ -131,9 +148,9 @@ static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bo
     p.out_vec = vec;
   }
   cudaError_t e;
-  if (p.a_planes == 1 && p.b_planes == 1) e = start_gemm<kEpi, tc::GEMM_ONE>(p, ma, mb, kind, st);
-  else if (p.a_planes == 2 && p.b_planes == 2) e = start_gemm<kEpi, tc::GEMM_SPLIT>(p, ma, mb, kind, st);
-  else if constexpr (kEpi != tc::EPI_CE) e = start_gemm<kEpi, tc::GEMM_LOW>(p, ma, mb, kind, st);
+  if (p.a_planes == 1 && p.b_planes == 1) e = start_gemm<kEpi, tc::GEMM_ONE>(p, ma, mb, cut, st);
+  else if (p.a_planes == 2 && p.b_planes == 2) e = start_gemm<kEpi, tc::GEMM_SPLIT>(p, ma, mb, cut, st);
+  else if constexpr (kEpi != tc::EPI_CE) e = start_gemm<kEpi, tc::GEMM_LOW>(p, ma, mb, cut, st);
   else return LP_ERR_UNSUPPORTED;
   LP_CUDA_OK(e);
   return LP_OK;

@@ -125,13 +125,26 @@ __device__ __forceinline__ void split_half(float v, __half& hi, __half& lo) {
   hi = __float2half_rn(v);
   lo = __float2half_rn(v - __half2float(hi));
 }
-__device__ __forceinline__ uint32_t pack_half2(__half a, __half b) {
-  return (uint32_t)__half_as_ushort(a) | ((uint32_t)__half_as_ushort(b) << 16);
-}
 __device__ __forceinline__ void half2_floats(uint32_t u, float& a, float& b) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
   a = f.x;
   b = f.y;
+}
+__device__ __forceinline__ uint32_t pack_half2(__half a, __half b) {
+  return (uint32_t)__half_as_ushort(a) | ((uint32_t)__half_as_ushort(b) << 16);
+}
+// Two at once (one instruction; converting one value at a time runs at an eighth of the rate).
+__device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Both parts of two values.
+__device__ __forceinline__ void split_f16x2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  hi = pack_f16x2(a, b);
+  float ha, hb;
+  half2_floats(hi, ha, hb);
+  lo = pack_f16x2(a - ha, b - hb);
 }
 
 // 32-byte global accesses (addresses are 32-byte aligned): a thread has a row of the accumulator, and what it reads or writes of
@@ -186,10 +199,13 @@ __device__ __forceinline__ void epi_h16(const GemmParams& p, int b, int row, int
     uint32_t h[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const __half h0 = __float2half_rn(v[2 * i]), h1 = __float2half_rn(v[2 * i + 1]);
-      h[i] = pack_half2(h0, h1);
-      v[2 * i] -= __half2float(h0);       // what the low part holds
-      v[2 * i + 1] -= __half2float(h1);
+      h[i] = pack_f16x2(v[2 * i], v[2 * i + 1]);
+      if (p.h_plane) {       // what is left for the low part
+        float a, b2;
+        half2_floats(h[i], a, b2);
+        v[2 * i] -= a;
+        v[2 * i + 1] -= b2;
+      }
     }
     st_v8(out + (long long)row * p.h_ld + col, h);
     st_v8(out + (long long)row * p.h_ld + col + 16, h + 8);
@@ -300,21 +316,24 @@ __device__ __forceinline__ void epi_out_any(const GemmParams& p, int b, int row0
   else rows_to((float*)p.out + at, p.out_ld, rows, scratch, p.update, p.keep, p.step);
 }
 
-// Logits of a 32-column group: scale, bias, and -inf past the last class.
-__device__ __forceinline__ void ce_logits(const GemmParams& p, int col, float f, int lane, float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 32; ++j) v[j] *= f;
+// Logits of a 32-column group: scale, bias (lane j's `bias` is of column `col` + j), and -inf past the last class.
+__device__ __forceinline__ void ce_logits(const GemmParams& p, int col, float f, float bias, float (&v)[32]) {
   if (p.bias) {
-    float bl = 0.f;
-    if (col + lane < p.N) bl = p.bias_bf16 ? __bfloat162float(((const bf16*)p.bias)[col + lane]) : ((const float*)p.bias)[col + lane];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bl, j);
+    for (int j = 0; j < 32; ++j) v[j] = fmaf(f, v[j], __shfl_sync(0xffffffffu, bias, j));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] *= f;
   }
   if (col + 32 > p.N) {
 #pragma unroll
     for (int j = 0; j < 32; ++j)
       if (col + j >= p.N) v[j] = -INFINITY;
   }
+}
+__device__ __forceinline__ float ce_bias(const GemmParams& p, int col) {
+  if (!p.bias || col >= p.N) return 0.f;
+  return p.bias_bf16 ? __bfloat162float(((const bf16*)p.bias)[col]) : ((const float*)p.bias)[col];
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -332,7 +351,7 @@ enum GemmMode {
 enum GemmKind {
   GEMM_SINGLE = 0,   // 128 x 128 by one CTA
   GEMM_PAIR = 1,     // 256 x 256 by a CTA pair
-  GEMM_KSPLIT = 2,   // 128 x 128 by a cluster of four CTAs, a quarter of K each; one tile a cluster
+  GEMM_KSPLIT = 2,   // 128 x 128 by a cluster of two to four CTAs, a share of K each; one tile a cluster
 };
 
 template <int kEpi, int kKind, int kMode>
@@ -345,13 +364,15 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   volatile int* abort_flag = &tail->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr bool kPair = kKind == GEMM_PAIR, kKSplit = kKind == GEMM_KSPLIT;
-  constexpr int kCtas = kPair ? 2 : 1, kCluster = kKSplit ? 4 : kCtas;
+  constexpr int kCtas = kPair ? 2 : 1;
+  constexpr bool kCluster = kPair || kKSplit;
   constexpr int kTileM = 128 * kCtas, kTileN = 128 * kCtas;
   constexpr uint32_t kAccCols = kTileN, kTmem = 2 * kAccCols;
-  const uint32_t crank = kCluster > 1 ? cluster_ctarank() : 0;
+  const uint32_t crank = kCluster ? cluster_ctarank() : 0;
   const uint32_t rank = kPair ? crank : 0;      // of the CTAs that share a tile's rows
   const bool leader = rank == 0;
-  const int unit = blockIdx.x / kCluster, units = gridDim.x / kCluster;
+  const int ctas = kKSplit ? (int)cluster_nctas() : kCtas;
+  const int unit = blockIdx.x / ctas, units = gridDim.x / ctas;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kGemmStages; ++s) {
@@ -378,14 +399,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   }
   tc_fence_before();
   __syncthreads();
-  if constexpr (kCluster > 1) cluster_sync_all();   // both CTAs' barriers exist before anything signals them from the other side
+  if constexpr (kCluster) cluster_sync_all();   // both CTAs' barriers exist before anything signals them from the other side
   tc_fence_after();
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t tmem_base = tail->tmem_base;
-  // (a quarter of K: at least one K block, see gemm_kind)
-  const int k_first = kKSplit ? p.kblocks * (int)crank / 4 : 0;
-  const int steps = kKSplit ? p.kblocks * (int)(crank + 1) / 4 - k_first : p.kblocks;
+  // (its share of K: at least one K block, see gemm_kind)
+  const int k_first = kKSplit ? p.kblocks * (int)crank / ctas : 0;
+  const int steps = kKSplit ? p.kblocks * (int)(crank + 1) / ctas - k_first : p.kblocks;
   constexpr bool kRounds = kMode == GEMM_SPLIT;
   const int round_len = kRounds ? p.round_len : steps;
   constexpr uint32_t kTiles = 2 + kMode, kStages = 12 / kTiles, kStageBytes = kTiles * kGemmTileBytes;
@@ -498,6 +519,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const int row0 = tm * kTileM + (int)rank * 128 + q * 32, row = row0 + lane;
       int col0 = tn * kTileN + half * (kTileN / 2);
       const float f = gemm_scale(p, b);
+      // (read while the products are under way)
+      float bias[kGroups] = {};
+      int label = -1;
+      if constexpr (kEpi == EPI_CE) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) bias[g] = ce_bias(p, col0 + g * 32 + lane);
+        if (row < p.M) label = p.labels[row];
+      }
       float acc[kRounds ? kGroups : 1][32];
       if constexpr (kRounds) {
 #pragma unroll
@@ -541,35 +570,41 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
       }
       if constexpr (kKSplit) {
-        // Each CTA of the cluster finishes one group of 32 columns: the other three send it their sums, into its ring (its own
-        // products have read it: the first barrier).  The warps that have the CTA's group add them up and go on with it.
+        // Group g of 32 columns is finished by CTA g % c: the others send it their sums, into its ring (its own products have read
+        // it: the first barrier).  The warps that have the group add them up, in the CTAs' order, and go on with it.
         float* ring = reinterpret_cast<float*>(smem);
+        const int c = (int)cluster_nctas();
         cluster_sync_all();
-        if (!failed) {
+        int mine = -1;
 #pragma unroll 1
-          for (int g = 0; g < kGroups; ++g) {
-            const uint32_t to = half * kGroups + g;
-            if (to == crank) continue;
+        for (int g = 0; g < kGroups; ++g) {
+          const int to = (half * kGroups + g) % c, slot = (half * kGroups + g) / c;
+          if (to == (int)crank) {
+            mine = g;
+          } else if (!failed) {
             float v[32];
             tmem_ld32(taddr + g * 32, v);
-            const uint32_t at = mapa_u32(smem_u32(ring + (crank * 32) * 128 + q * 32 + lane), to);
+            const uint32_t at = mapa_u32(smem_u32(ring + ((slot * c + (int)crank) * 32) * 128 + q * 32 + lane), to);
 #pragma unroll
             for (int j = 0; j < 32; ++j) st_cluster_f32(at + j * 512, v[j]);
           }
         }
         cluster_sync_all();
-        const int mine = (int)crank - half * kGroups;
-        if (failed || mine < 0 || mine >= kGroups) break;
+        if (failed || mine < 0) break;
+        const int slot = (half * kGroups + mine) / c;
         taddr += mine * 32;
-        float v[32];
-        tmem_ld32(taddr, v);
-        for (int r = 0; r < 4; ++r)
-          if (r != (int)crank) {
+        col0 += mine * 32;
+        if (mine) bias[0] = bias[kGroups - 1];
+        float own[32], v[32];
+        tmem_ld32(taddr, own);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] += ring[(r * 32 + j) * 128 + q * 32 + lane];
-          }
+        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+        for (int r = 0; r < c; ++r) {
+          const float* from = ring + ((slot * c + r) * 32) * 128 + q * 32 + lane;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] += r == (int)crank ? own[j] : from[j * 128];
+        }
         tmem_st32(taddr, v);
-        col0 = tn * kTileN + (int)crank * 32;
         groups = 1;
       }
       if constexpr (kEpi == EPI_CE) {
@@ -578,12 +613,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         for (int g = 0; g < groups; ++g) {
           float v[32];
           tmem_ld32(taddr + g * 32, v);
-          ce_logits(p, col0 + g * 32, f, lane, v);
+          ce_logits(p, col0 + g * 32, f, g == 0 ? bias[0] : g == 1 ? bias[1] : g == 2 ? bias[kGroups > 2 ? 2 : 0] : bias[kGroups > 2 ? 3 : 0], v);
 #pragma unroll
           for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
         }
         const float ref = top == -INFINITY ? 0.f : top;   // a half without any class counts nothing
-        const int label = row < p.M ? p.labels[row] : -1;
         float sum = 0.f;
 #pragma unroll 1
         for (int g = 0; g < groups; ++g) {
@@ -591,7 +625,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           float v[32];
           tmem_ld32(taddr + g * 32, v);
           if (g + 1 == groups) release();
-          ce_logits(p, col, f, lane, v);
+          ce_logits(p, col, f, g == 0 ? bias[0] : g == 1 ? bias[1] : g == 2 ? bias[kGroups > 2 ? 2 : 0] : bias[kGroups > 2 ? 3 : 0], v);
           if (label >= col && label < col + 32) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
@@ -604,7 +638,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
           if (p.h_out && col < p.N) epi_h16(p, 0, row, col, false, v);
         }
-        if (row < p.M) p.stats[(long long)(kKSplit ? tn * 4 + (int)crank : tn * 2 + half) * p.stats_ld + row] = make_float2(ref, sum * 6.103515625e-5f);
+        if (row < p.M) p.stats[(long long)(col0 / (kKSplit ? 32 : kTileN / 2)) * p.stats_ld + row] = make_float2(ref, sum * 6.103515625e-5f);
       } else {
         const bool mirror = p.sym && tm != tn;
 #pragma unroll 1
@@ -647,7 +681,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll 1
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
   }
-  if constexpr (kCluster > 1) cluster_sync_all();   // no CTA leaves while another may still signal it or write its ring
+  if constexpr (kCluster) cluster_sync_all();   // no CTA leaves while another may still signal it or write its ring
   if (warp == 2) {
     tc_fence_after();
     if constexpr (kPair) tmem2_dealloc(tmem_base, kTmem);

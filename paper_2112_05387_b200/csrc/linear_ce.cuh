@@ -148,30 +148,40 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int
         ((bf16*)dst)[at] = keep ? ((const bf16*)src)[from] : __float2bfloat16_rn(0.f);
       }
     } else {
-      __half hi[N], lo[N];
-      float v[N];
       if constexpr (kVec) {
-        float a[4], b[4];
-        ldv((const float*)src + from, a);
-        ldv((const float*)src + from + 4, b);
+        float v[4], z[4];
+        uint32_t hi[4], lo[4];
+        ldv((const float*)src + from, v);
+        ldv((const float*)src + from + 4, z);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[4 + j] = b[j]; }
+        for (int j = 0; j < 2; ++j) {
+          tc::split_f16x2(keep ? v[2 * j] * scale : 0.f, keep ? v[2 * j + 1] * scale : 0.f, hi[j], lo[j]);
+          tc::split_f16x2(keep ? z[2 * j] * scale : 0.f, keep ? z[2 * j + 1] * scale : 0.f, hi[2 + j], lo[2 + j]);
+        }
+        *reinterpret_cast<uint4*>(dst + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(dst + plane + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       } else {
-        v[0] = ((const float*)src)[from];
-      }
-#pragma unroll
-      for (int j = 0; j < N; ++j) tc::split_half(keep ? v[j] * scale : 0.f, hi[j], lo[j]);
-      if constexpr (kVec) {
-        *reinterpret_cast<uint4*>(dst + at) = make_uint4(tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]),
-                                                         tc::pack_half2(hi[4], hi[5]), tc::pack_half2(hi[6], hi[7]));
-        *reinterpret_cast<uint4*>(dst + plane + at) = make_uint4(tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]),
-                                                                 tc::pack_half2(lo[4], lo[5]), tc::pack_half2(lo[6], lo[7]));
-      } else {
-        dst[at] = hi[0];
-        dst[plane + at] = lo[0];
+        __half hi, lo;
+        tc::split_half(keep ? ((const float*)src)[from] * scale : 0.f, hi, lo);
+        dst[at] = hi;
+        dst[plane + at] = lo;
       }
     }
   }
+}
+
+// Joins a part (maximum, sum of exponentials relative to it) to another.  A part without any class has the sum 0, and its
+// reference says nothing; an infinite logit makes the sum NaN, as inf - inf is.
+__device__ __forceinline__ void ce_join(float& m, float& s, const float2 v) {
+  if (v.y == 0.f) return;
+  if (s == 0.f) {
+    m = v.x;
+    s = v.x == INFINITY ? NAN : v.y;
+    return;
+  }
+  const float top = fmaxf(m, v.x);
+  s = s * exp2f((m - top) * tc::kLog2e) + v.y * exp2f((v.x - top) * tc::kLog2e);
+  m = top;
 }
 
 // lse and loss of each row from its parts: 8 rows a block (32 bytes of each part), 32 threads a row.
@@ -184,27 +194,132 @@ ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, 
   float m = -INFINITY, s = 0.f;
   if (row < rows) {
 #pragma unroll 4
-    for (int i = y; i < parts; i += 32) {
-      const float2 v = stats[(long long)i * stats_ld + row];
-      if (v.y == 0.f) continue;              // a part without any class (its reference says nothing)
-      const float top = fmaxf(m, v.x);
-      if (top == INFINITY) { m = top; s = NAN; continue; }
-      s = s * exp2f((m - top) * tc::kLog2e) + v.y * exp2f((v.x - top) * tc::kLog2e);
-      m = top;
-    }
+    for (int i = y; i < parts; i += 32) ce_join(m, s, stats[(long long)i * stats_ld + row]);
   }
   __shared__ float ms[32][8], ss[32][8];
   ms[y][r] = m;
   ss[y][r] = s;
   __syncthreads();
   if (y || row >= rows) return;
-  for (int i = 1; i < 32; ++i) m = fmaxf(m, ms[i][r]);
-  float sum = 0.f;
-  for (int i = 0; i < 32; ++i)
-    if (ss[i][r] != 0.f) sum += ss[i][r] * exp2f((ms[i][r] - m) * tc::kLog2e);
-  const float l = m + logf(sum);
+  for (int i = 1; i < 32; ++i) ce_join(m, s, make_float2(ms[i][r], ss[i][r]));
+  const float l = m + logf(s);
   lse[row] = l;
   row_loss[row] = ce_counts(labels[row], V) ? l - target[row] : 0.f;
+}
+
+// All of it at once for few rows and parts, in one block: lse and loss of each row, a warp each, the number of counted rows and
+// the mean.
+__global__ void __launch_bounds__(1024)
+ce_finish_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, int rows, int V, const int32_t* __restrict__ labels,
+                 const float* __restrict__ target, float* __restrict__ lse, float* __restrict__ row_loss, float* __restrict__ loss) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  double total = 0.0;
+  int count = 0;
+  for (int row = warp; row < rows; row += 32) {
+    float m = -INFINITY, s = 0.f;
+#pragma unroll 4
+    for (int i = lane; i < parts; i += 32) ce_join(m, s, stats[(long long)i * stats_ld + row]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float2 v = make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
+      // (both lanes of an exchange add the same two terms, the lower lane's first: the same bits)
+      float a = lane & o ? v.x : m, b = lane & o ? v.y : s;
+      ce_join(a, b, lane & o ? make_float2(m, s) : v);
+      m = a;
+      s = b;
+    }
+    const float l = m + logf(s);
+    const bool counts = ce_counts(labels[row], V);
+    const float x = counts ? l - target[row] : 0.f;
+    if (lane == 0) {
+      lse[row] = l;
+      row_loss[row] = x;
+    }
+    total += (double)x;
+    count += counts;
+  }
+  __shared__ double totals[32];
+  __shared__ int counts_s[32];
+  if (lane == 0) {
+    totals[warp] = total;
+    counts_s[warp] = count;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 32; ++w) {
+      total += totals[w];
+      count += counts_s[w];
+    }
+    loss[0] = count > 0 ? (float)(total / count) : 0.f;
+    loss[1] = (float)count;
+  }
+}
+
+// Loss alone of at most four rows: a pass over w that its bytes bound (a tile of the tensor cores holds 128 rows, and fetches w
+// in rows of 128 bytes: 105 us for one row, 2048 x 100000 in bf16, 64 us of bytes).  A warp has four classes at a time, each lane 16 bytes of each of
+// them a step; x stands in shared memory in fp32.  Every block joins its warps' maxima and sums to one part.
+template <typename T, int kRows, bool kVec>
+__global__ void __launch_bounds__(kCeThreads)
+ce_few_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __restrict__ bias, const int32_t* __restrict__ labels, int rows, int D,
+              int V, float2* __restrict__ stats, long long stats_ld, float* __restrict__ target, CeHeader* __restrict__ hdr) {
+  extern __shared__ __align__(16) float few_x[];   // [kRows][D]
+  pdl_wait();
+  pdl_launch_dependents();
+  if (blockIdx.x == 0 && threadIdx.x == 0) hdr->err = 0;
+  for (int i = threadIdx.x; i < kRows * D; i += kCeThreads) few_x[i] = i < rows * D ? to_f(x[i]) : 0.f;
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int N = kVec ? VecT<T>::N : 1;
+  float m[kRows], s[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) { m[r] = -INFINITY; s[r] = 0.f; }
+  for (int v0 = (blockIdx.x * 8 + warp) * 4; v0 < V; v0 += gridDim.x * 32) {
+    const T* at[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) at[c] = w + (long long)min(v0 + c, V - 1) * D;
+    float acc[4][kRows] = {};
+#pragma unroll 2
+    for (int d = lane * N; d < D; d += 32 * N) {
+      float f[4][N];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if constexpr (kVec) ldv(at[c] + d, f[c]);
+        else f[c][0] = to_f(at[c][d]);
+      }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float xv = few_x[r * D + d + j];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c][r] = fmaf(f[c][j], xv, acc[c][r]);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (v0 + c >= V) break;
+      const float b = bias ? to_f(bias[v0 + c]) : 0.f;
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const float l = warp_sum(acc[c][r]) + b;
+        if (r < rows && lane == 0 && labels[r] == v0 + c) target[r] = l;
+        if (l == -INFINITY) continue;
+        ce_join(m[r], s[r], make_float2(l, 1.f));
+      }
+    }
+  }
+  __shared__ float2 parts[8][kRows];
+  if (lane == 0)
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) parts[warp][r] = make_float2(m[r], s[r]);
+  __syncthreads();
+  if (threadIdx.x < rows) {
+    float a = -INFINITY, b = 0.f;
+    for (int i = 0; i < 8; ++i) ce_join(a, b, parts[i][threadIdx.x]);
+    stats[(long long)blockIdx.x * stats_ld + threadIdx.x] = make_float2(a, b);
+  }
 }
 
 // Mean over the counted rows: one block, always in the same order.
@@ -227,74 +342,85 @@ ce_loss_kernel(const float* __restrict__ row_loss, int T, const CeHeader* __rest
   }
 }
 
-// Exponentials -> dl (without the factor g / count), in place, and the column sums of a slab of rows for dbias.
-// A thread has 8 columns; `part_cols` columns share a reference in `stats`.
+// Exponentials -> dl (without the factor g / count), in place, and the column sums of a slab of rows for dbias: the block's slab in
+// `sums`, or dbias itself where one slab is all there is.  A warp has 256 columns of every eighth row, a thread 8 of them;
+// `part_cols` columns share a reference in `stats`.
+constexpr int kCeSlab = 64;
 template <bool kF32>
 __global__ void __launch_bounds__(kCeThreads)
-ce_dl_kernel(__half* __restrict__ p, long long ld, long long plane, int rows, int V, int slab, const float2* __restrict__ stats,
-             long long stats_ld, int part_cols, const float* __restrict__ lse, const float* __restrict__ target,
-             const int32_t* __restrict__ labels, float* __restrict__ sums /* [slab][V] or null */) {
+ce_dl_kernel(__half* __restrict__ p, long long ld, long long plane, int rows, int V, const float2* __restrict__ stats, long long stats_ld,
+             int part_cols, const float* __restrict__ lse, const float* __restrict__ target, const int32_t* __restrict__ labels,
+             float* __restrict__ sums /* [slab][V] or null */, void* __restrict__ dbias /* or null */, const CeHeader* __restrict__ hdr) {
   pdl_wait();
   pdl_launch_dependents();
-  const int col = (blockIdx.x * kCeThreads + threadIdx.x) * 8;
-  if (col >= V) return;
-  const float2* ref = stats + (long long)(col / part_cols) * stats_ld;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int col = blockIdx.x * 256 + lane * 8;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const int r1 = min(rows, (int)(blockIdx.y + 1) * slab);
-  for (int r = blockIdx.y * slab; r < r1; ++r) {
-    const int label = labels[r];
-    __half* q = p + (long long)r * ld + col;
-    float v[8];
-    if (ce_counts(label, V)) {
-      const float f = exp2f(fmaf(ref[r].x - lse[r], tc::kLog2e, -tc::kCeExpBits));
+  if (col < V) {
+    const float2* ref = stats + (long long)(col / part_cols) * stats_ld;
+    const int r1 = min(rows, (int)(blockIdx.y + 1) * kCeSlab);
+#pragma unroll 2
+    for (int r = blockIdx.y * kCeSlab + warp; r < r1; r += 8) {
+      const int label = labels[r];
+      __half* q = p + (long long)r * ld + col;
+      float v[8];
       const uint4 h = *reinterpret_cast<const uint4*>(q);
-      const uint32_t u[4] = {h.x, h.y, h.z, h.w};
+      uint4 l = make_uint4(0u, 0u, 0u, 0u);
+      if constexpr (kF32) l = *reinterpret_cast<const uint4*>(q + plane);
+      if (ce_counts(label, V)) {
+        const float f = exp2f(fmaf(ref[r].x - lse[r], tc::kLog2e, -tc::kCeExpBits));
+        const uint32_t u[4] = {h.x, h.y, h.z, h.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tc::half2_floats(u[i], v[2 * i], v[2 * i + 1]);
-      if constexpr (kF32) {
-        const uint4 l = *reinterpret_cast<const uint4*>(q + plane);
-        const uint32_t w[4] = {l.x, l.y, l.z, l.w};
+        for (int i = 0; i < 4; ++i) tc::half2_floats(u[i], v[2 * i], v[2 * i + 1]);
+        if constexpr (kF32) {
+          const uint32_t w[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float a, b;
-          tc::half2_floats(w[i], a, b);
-          v[2 * i] += a;
-          v[2 * i + 1] += b;
+          for (int i = 0; i < 4; ++i) {
+            float a, b;
+            tc::half2_floats(w[i], a, b);
+            v[2 * i] += a;
+            v[2 * i + 1] += b;
+          }
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= f;
+        if (label >= col && label < col + 8) {
+          const float d = expm1f(target[r] - lse[r]);   // p - 1 without the cancellation
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (col + j == label) v[j] = d;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.f;
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= f;
-      if (label >= col && label < col + 8) {
-        const float d = expm1f(target[r] - lse[r]);   // p - 1 without the cancellation
+      for (int j = 0; j < 8; ++j) acc[j] += v[j];
+      if constexpr (kF32) {
+        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (col + j == label) v[j] = d;
+        for (int j = 0; j < 4; ++j) tc::split_f16x2(v[2 * j] * kCeDlScale, v[2 * j + 1] * kCeDlScale, hi[j], lo[j]);
+        *reinterpret_cast<uint4*>(q) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(q + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      } else {
+        *reinterpret_cast<uint4*>(q) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                                  pack_bf16x2(v[6], v[7]));
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] += v[j];
-    if constexpr (kF32) {
-      __half hi[8], lo[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) tc::split_half(v[j] * kCeDlScale, hi[j], lo[j]);
-      *reinterpret_cast<uint4*>(q) = make_uint4(tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]),
-                                                tc::pack_half2(hi[4], hi[5]), tc::pack_half2(hi[6], hi[7]));
-      *reinterpret_cast<uint4*>(q + plane) = make_uint4(tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]),
-                                                        tc::pack_half2(lo[4], lo[5]), tc::pack_half2(lo[6], lo[7]));
-    } else {
-      *reinterpret_cast<uint4*>(q) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                                                pack_bf16x2(v[6], v[7]));
     }
   }
-  if (sums) {
-    float* s = sums + (long long)blockIdx.y * V + col;
+  if (!sums && !dbias) return;
+  __shared__ float part[8][256];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (col + j < V) s[j] = acc[j];
-  }
+  for (int j = 0; j < 8; ++j) part[warp][lane * 8 + j] = acc[j];
+  __syncthreads();
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= V) return;
+  float s = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) s += part[w][threadIdx.x];
+  if (sums) sums[(long long)blockIdx.y * V + c] = s;
+  else if (kF32) ((float*)dbias)[c] = s * hdr->grad_f;
+  else ((bf16*)dbias)[c] = __float2bfloat16_rn(s * hdr->grad_f);
 }
 
 // dbias from the slabs' column sums.

@@ -167,8 +167,8 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   }
   if ((rc = encode_gemm_map(&m_a, GemmOperand{s.a, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
   if ((rc = encode_gemm_map(&m_b, GemmOperand{s.b, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
-  const tc::GemmKind kind_g = gemm_kind(small, small, tall ? q.rows : q.cols, B, true, planes, planes),
-                     kind_a = gemm_kind(small, small, small, B, true, planes, planes);
+  const GemmCut cut_g = gemm_cut(small, small, tall ? q.rows : q.cols, B, true, planes, planes),
+                     cut_a = gemm_cut(small, small, small, B, true, planes, planes);
 
   int cur = 0;
   for (int i = 0; i < q.steps; ++i) {
@@ -181,8 +181,8 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.f = first ? kScaleA : kScaleA / (kScaleX * kScaleX);
     p.f_dev = s.alpha; p.f_pow = first ? 2 : 0;
     p.h_out = s.a; p.h_ld = s.ld_s; p.h_batch = s_mat; p.h_plane = q.split ? s_plane : 0;
-    if (tall) rc = launch_gemm<tc::EPI_H16>(p, q.rows, m_xm[cur], true, m_xm[cur], true, false, kind_g, st);
-    else rc = launch_gemm<tc::EPI_H16>(p, q.cols, m_xk[cur], false, m_xk[cur], false, false, kind_g, st);
+    if (tall) rc = launch_gemm<tc::EPI_H16>(p, q.rows, m_xm[cur], true, m_xm[cur], true, false, cut_g, st);
+    else rc = launch_gemm<tc::EPI_H16>(p, q.cols, m_xk[cur], false, m_xk[cur], false, false, cut_g, st);
     if (rc != LP_OK) return rc;
     // B = a I + b A + c A^2
     memset(&p, 0, sizeof(p));
@@ -191,7 +191,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.f = q.coeffs[2] * (kScaleB / (kScaleA * kScaleA));
     p.h_out = s.b; p.h_ld = s.ld_s; p.h_batch = s_mat; p.h_plane = q.split ? s_plane : 0;
     p.aux = s.a; p.aux_f = q.coeffs[1] * (kScaleB / kScaleA); p.diag = q.coeffs[0] * kScaleB;
-    rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, kind_a, st);
+    rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, cut_a, st);
     if (rc != LP_OK) return rc;
     // X <- B X (X B).  An error in X grows by up to a in each later step, so its low part is kept while three or more
     // products follow (relative error of the result, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3 with the
@@ -202,7 +202,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.b_planes = tall ? planes : x_planes;
     p.f = last ? 1.f / (first ? kScaleB : kScaleB * kScaleX) : (first ? kScaleX / kScaleB : 1.f / kScaleB);
     p.f_dev = s.alpha; p.f_pow = first ? 1 : 0;
-    const tc::GemmKind kind_x = gemm_kind(q.rows, q.cols, small, B, false, p.a_planes, p.b_planes);
+    const GemmCut cut_x = gemm_cut(q.rows, q.cols, small, B, false, p.a_planes, p.b_planes);
     const CUtensorMap& ma = tall ? m_xk[cur] : m_b;
     const CUtensorMap& mb = tall ? m_b : m_xm[cur];
     if (last) {
@@ -212,12 +212,12 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
         p.use_off = 1;
         for (int b = 0; b < B; ++b) p.off[b] = q.off[b];
       }
-      rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, kind_x, st);
+      rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, cut_x, st);
     } else {
       x_planes = (q.split || i + 3 < q.steps) ? 2 : 1;
       cur ^= 1;
       p.h_out = s.x[cur]; p.h_ld = s.ld; p.h_batch = x_mat; p.h_plane = x_planes == 2 ? x_plane : 0;
-      rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, kind_x, st);
+      rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, cut_x, st);
     }
     if (rc != LP_OK) return rc;
     n += 3;
@@ -243,6 +243,8 @@ static int check_ortho(int dtype, int batch, int rows, int cols, int steps, floa
 // one piece.
 static const size_t kCePieceBytes = (size_t)512 << 20;
 static const int kCeAmaxParts = 592;
+static const int kCeFewBlocks = 296;        // two an SM
+static const size_t kCeFewSmem = 96 * 1024;
 
 struct CeScratch {
   CeHeader* hdr;
@@ -251,7 +253,6 @@ struct CeScratch {
   __half *p, *x, *w;
   long long ld_v, ld_d;
   int rows;                        // of a piece
-  int slab;
   bool f32, pack_w;
 };
 static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) {
@@ -266,23 +267,61 @@ static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) 
   const bool whole = grads && !s.f32 && (size_t)T * row_bytes <= (size_t)V * D * 4;
   const long long fit = whole ? T : (long long)(kCePieceBytes / row_bytes) / 256 * 256;
   s.rows = (int)std::min<long long>(T, std::min(std::max(256LL, fit), 1LL << 18));
-  // rows of a block of the pass over the exponentials: 64, fewer where that leaves SMs idle
-  s.slab = 64;
-  const long long col_blocks = (V + kCeThreads * 8 - 1) / (kCeThreads * 8);
-  while (s.slab > 4 && col_blocks * ((s.rows + s.slab - 1) / s.slab) < 592) s.slab /= 2;
   s.hdr = c.take<CeHeader>(1);
   s.amax = c.take<float>(2 * kCeAmaxParts);
   s.target = c.take<float>(T);
   s.lse = c.take<float>(T);
   s.row_loss = c.take<float>(T);
-  s.stats = c.take<float2>((size_t)4 * ((V + 127) / 128) * s.rows);
+  s.stats = c.take<float2>((size_t)std::max(4 * ((V + 127) / 128), kCeFewBlocks) * s.rows);
   const bool pack_x = s.pack_w || grads;
   s.x = pack_x ? c.take<__half>((size_t)planes * T * s.ld_d) : nullptr;
   s.w = s.pack_w ? c.take<__half>((size_t)planes * V * s.ld_d) : nullptr;
   s.p = grads ? c.take<__half>((size_t)planes * s.rows * s.ld_v) : nullptr;
-  s.sums = grads ? c.take<float>((size_t)((T + s.slab - 1) / s.slab + T / s.rows + 1) * V) : nullptr;
+  s.sums = grads ? c.take<float>((size_t)(T / kCeSlab + T / s.rows + 2) * V) : nullptr;
   s.acc = grads && !s.f32 && s.rows < T ? c.take<float>((size_t)V * D) : nullptr;
   return s;
+}
+
+// Loss alone of a few rows.
+static const int kCeFewRows = 4;
+template <typename T, int kRows>
+static int start_few(const CeScratch& s, int rows, int D, int V, const T* x, const T* w, const T* bias, const int32_t* labels, int blocks,
+                     cudaStream_t st) {
+  const size_t smem = (size_t)kRows * D * 4;
+  LP_CUDA_OK(launch_pdl(D % VecT<T>::N ? ce_few_kernel<T, kRows, false> : ce_few_kernel<T, kRows, true>, dim3(blocks), dim3(kCeThreads), smem,
+                        st, x, w, bias, labels, rows, D, V, s.stats, (long long)s.rows, s.target, s.hdr));
+  return LP_OK;
+}
+template <typename T>
+static int ce_few_rows(const CeScratch& s, int rows, int D, int V, const T* x, const T* w, const T* bias, const int32_t* labels, float* row_loss,
+                       float* loss, cudaStream_t st) {
+  const int blocks = (int)std::min<long long>(std::min(kCeFewBlocks, 2 * cur_dev().sm_count), (V + 31) / 32);
+  const int rc = rows == 1 ? start_few<T, 1>(s, rows, D, V, x, w, bias, labels, blocks, st)
+                 : rows == 2 ? start_few<T, 2>(s, rows, D, V, x, w, bias, labels, blocks, st)
+                             : start_few<T, 4>(s, rows, D, V, x, w, bias, labels, blocks, st);
+  if (rc != LP_OK) return rc;
+  LP_CUDA_OK(launch_pdl(ce_finish_kernel, dim3(1), dim3(1024), 0, st, (const float2*)s.stats, (long long)s.rows, blocks, rows, V, labels,
+                        (const float*)s.target, s.lse, row_loss, loss));
+  return LP_OK;
+}
+template <typename T, int kRows>
+static int few_set_attributes() {
+  LP_CUDA_OK(cudaFuncSetAttribute(ce_few_kernel<T, kRows, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCeFewSmem));
+  LP_CUDA_OK(cudaFuncSetAttribute(ce_few_kernel<T, kRows, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCeFewSmem));
+  return LP_OK;
+}
+static int ce_init_dev() {
+  int rc = gemm_init_dev();
+  if (rc != LP_OK) return rc;
+  std::lock_guard<std::mutex> lock(g_devices_mutex);
+  Device& D = cur_dev();
+  if (D.ce_attr) return LP_OK;
+  if ((rc = few_set_attributes<float, 1>()) != LP_OK || (rc = few_set_attributes<float, 2>()) != LP_OK ||
+      (rc = few_set_attributes<float, 4>()) != LP_OK || (rc = few_set_attributes<bf16, 1>()) != LP_OK ||
+      (rc = few_set_attributes<bf16, 2>()) != LP_OK || (rc = few_set_attributes<bf16, 4>()) != LP_OK)
+    return rc;
+  D.ce_attr = true;
+  return LP_OK;
 }
 
 }  // namespace lp
@@ -352,7 +391,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   if (reinterpret_cast<uintptr_t>(scratch) & 255) return LP_ERR_ALIGN;
   const bool grads = dx || dw || dbias;
   if (scratch_bytes < lp_linear_cross_entropy_scratch_bytes(dtype, T, D, V, grads)) return LP_ERR_WORKSPACE;
-  int rc = gemm_init_dev();
+  int rc = ce_init_dev();
   if (rc != LP_OK) return rc;
   const Device& Dv = cur_dev();
   cudaStream_t st = (cudaStream_t)stream;
@@ -361,6 +400,9 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   const int planes = s.f32 ? 2 : 1, is_bf16 = !s.f32;
   const long long x_plane = (long long)T * s.ld_d, w_plane = (long long)V * s.ld_d, p_plane = (long long)s.rows * s.ld_v;
   float* rl = row_loss ? row_loss : s.row_loss;
+  if (!grads && T <= kCeFewRows && (size_t)(T == 3 ? 4 : T) * D * 4 <= kCeFewSmem)
+    return s.f32 ? ce_few_rows(s, T, D, V, (const float*)x, (const float*)w, (const float*)bias, labels, rl, loss_out, st)
+                 : ce_few_rows(s, T, D, V, (const bf16*)x, (const bf16*)w, (const bf16*)bias, labels, rl, loss_out, st);
   const int amax_blocks = s.f32 ? 2 * kCeAmaxParts : 0;
   LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + amax_blocks), dim3(kCeThreads), 0, st, labels, T, V, (const float*)x, (long long)T * D,
                         (const float*)w, (long long)V * D, s.amax, kCeAmaxParts, s.hdr));
@@ -378,13 +420,14 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   if ((rc = encode_gemm_map(&m_wk, ow, false)) != LP_OK) return rc;
   if ((rc = encode_gemm_map(&m_wm, ow, true)) != LP_OK) return rc;
   int slab0 = 0;
+  bool finished = false, one_slab = false;
   for (int r0 = 0; r0 < T; r0 += s.rows) {
     const int rows = std::min(s.rows, T - r0);
     const GemmOperand ox{(const uint16_t*)xm + (long long)r0 * ldx, D, rows, ldx, x_plane, planes, !s.f32};
     CUtensorMap m_xk, m_xm, m_pk, m_pm;
     if ((rc = encode_gemm_map(&m_xk, ox, false)) != LP_OK) return rc;
-    const tc::GemmKind kind = gemm_kind(rows, V, D, 1, false, planes, planes);
-    const int part_cols = kind == tc::GEMM_PAIR ? 128 : kind == tc::GEMM_SINGLE ? 64 : 32;
+    const GemmCut cut = gemm_cut(rows, V, D, 1, false, planes, planes);
+    const int part_cols = cut.kind == tc::GEMM_PAIR ? 128 : cut.kind == tc::GEMM_SINGLE ? 64 : 32;
     const int parts = (V + part_cols - 1) / part_cols;
     tc::GemmParams p;
     memset(&p, 0, sizeof(p));
@@ -394,16 +437,22 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     p.bias = bias; p.bias_bf16 = is_bf16; p.labels = labels + r0;
     p.stats = s.stats; p.stats_ld = s.rows; p.target = s.target + r0;
     p.h_out = s.p; p.h_ld = s.ld_v; p.h_plane = s.f32 ? p_plane : 0;
-    if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, kind, st)) != LP_OK) return rc;
-    LP_CUDA_OK(launch_pdl(ce_rows_kernel, dim3((rows + 7) / 8), dim3(kCeThreads), 0, st, (const float2*)s.stats, (long long)s.rows, parts,
-                          rows, V, labels + r0, (const float*)(s.target + r0), s.lse + r0, rl + r0));
+    if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, cut, st)) != LP_OK) return rc;
+    // few rows and parts: one block does the rest of the loss
+    finished = rows == T && (long long)rows * parts <= 16384;
+    if (finished)
+      LP_CUDA_OK(launch_pdl(ce_finish_kernel, dim3(1), dim3(1024), 0, st, (const float2*)s.stats, (long long)s.rows, parts, rows, V, labels,
+                            (const float*)s.target, s.lse, rl, loss_out));
+    else
+      LP_CUDA_OK(launch_pdl(ce_rows_kernel, dim3((rows + 7) / 8), dim3(kCeThreads), 0, st, (const float2*)s.stats, (long long)s.rows, parts,
+                            rows, V, labels + r0, (const float*)(s.target + r0), s.lse + r0, rl + r0));
     if (!grads) continue;
-    const int slabs = (rows + s.slab - 1) / s.slab;
-    const dim3 gd((V + kCeThreads * 8 - 1) / (kCeThreads * 8), slabs);
-    float* sums = dbias ? s.sums + (long long)slab0 * V : nullptr;
-    LP_CUDA_OK(launch_pdl(s.f32 ? ce_dl_kernel<true> : ce_dl_kernel<false>, gd, dim3(kCeThreads), 0, st, s.p, s.ld_v, p_plane, rows, V, s.slab,
-                          (const float2*)s.stats, (long long)s.rows, part_cols, (const float*)(s.lse + r0), (const float*)(s.target + r0),
-                          labels + r0, sums));
+    const int slabs = (rows + kCeSlab - 1) / kCeSlab;
+    one_slab = slabs == 1 && rows == T;
+    float* sums = dbias && !one_slab ? s.sums + (long long)slab0 * V : nullptr;
+    LP_CUDA_OK(launch_pdl(s.f32 ? ce_dl_kernel<true> : ce_dl_kernel<false>, dim3((V + 255) / 256, slabs), dim3(kCeThreads), 0, st, s.p, s.ld_v,
+                          p_plane, rows, V, (const float2*)s.stats, (long long)s.rows, part_cols, (const float*)(s.lse + r0),
+                          (const float*)(s.target + r0), labels + r0, sums, one_slab ? dbias : nullptr, (const CeHeader*)s.hdr));
     slab0 += slabs;
     const GemmOperand op{s.p, V, rows, s.ld_v, p_plane, planes, !s.f32};
     if (dx) {
@@ -413,7 +462,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.a_planes = p.b_planes = planes;
       p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1;
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
-      const tc::GemmKind kd = gemm_kind(rows, D, V, 1, false, planes, planes);
+      const GemmCut kd = gemm_cut(rows, D, V, 1, false, planes, planes);
       if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, kd, st)) != LP_OK) return rc;
     }
     if (dw) {
@@ -429,14 +478,15 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
         p.acc_first = r0 == 0;
         p.acc_last = r0 + rows == T;
       }
-      const tc::GemmKind kd = gemm_kind(V, D, rows, 1, false, planes, planes);
+      const GemmCut kd = gemm_cut(V, D, rows, 1, false, planes, planes);
       if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, kd, st)) != LP_OK) return rc;
     }
   }
-  if (dbias)
+  if (dbias && !one_slab)
     LP_CUDA_OK(launch_pdl(ce_dbias_kernel, dim3((V + kCeThreads - 1) / kCeThreads), dim3(kCeThreads), 0, st, (const float*)s.sums, slab0, V,
                           (const CeHeader*)s.hdr, dbias, is_bf16));
-  LP_CUDA_OK(launch_pdl(ce_loss_kernel, dim3(1), dim3(kCeThreads), 0, st, (const float*)rl, T, (const CeHeader*)s.hdr, loss_out));
+  if (!finished)
+    LP_CUDA_OK(launch_pdl(ce_loss_kernel, dim3(1), dim3(kCeThreads), 0, st, (const float*)rl, T, (const CeHeader*)s.hdr, loss_out));
   return LP_OK;
 }
 

@@ -150,21 +150,20 @@ ortho_pack_kernel(const __grid_constant__ OrthoSource s, int parts, const double
       ortho_load<kVec>(s.momentum, 0, base + i * N, m);
       ortho_direction(s, u, m);
     }
-    __half hi[N], lo[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) tc::split_half(u[j] * scale, hi[j], lo[j]);
     // (a 64-bit division costs as much as the rest of the loop)
     const long long r = groups >> 32 ? i / per_row : (long long)((uint32_t)i / (uint32_t)per_row);
     __half* at = out + r * ld + (i - r * per_row) * N;
     if constexpr (kVec) {
-      *reinterpret_cast<uint4*>(at) = make_uint4(tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]), tc::pack_half2(hi[4], hi[5]),
-                                                 tc::pack_half2(hi[6], hi[7]));
-      if (x_plane)
-        *reinterpret_cast<uint4*>(at + x_plane) = make_uint4(tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]),
-                                                             tc::pack_half2(lo[4], lo[5]), tc::pack_half2(lo[6], lo[7]));
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) tc::split_f16x2(u[2 * j] * scale, u[2 * j + 1] * scale, hi[j], lo[j]);
+      *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      if (x_plane) *reinterpret_cast<uint4*>(at + x_plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     } else {
-      *at = hi[0];
-      if (x_plane) at[x_plane] = lo[0];
+      __half hi, lo;
+      tc::split_half(u[0] * scale, hi, lo);
+      *at = hi;
+      if (x_plane) at[x_plane] = lo;
     }
   }
 }

@@ -215,16 +215,16 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
         for (int r = 0; r < 8; ++r)
           if (r < q.ctas) { v[0] += x[r].x; v[1] += x[r].y; v[2] += x[r].z; v[3] += x[r].w; }
       }
-      __half hi[4], lo[4];
+      uint32_t hi[2], lo[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tc::split_half(v[i] * (kA / (kX * kX)), hi[i], lo[i]);
+      for (int i = 0; i < 2; ++i) tc::split_f16x2(v[2 * i] * (kA / (kX * kX)), v[2 * i + 1] * (kA / (kX * kX)), hi[i], lo[i]);
       const uint32_t at = tc::smem_u32(A + e / S * LD + e % S);
 #pragma unroll
       for (int r = 0; r < 8; ++r)
         if (r < q.ctas) {
           const uint32_t to = tc::mapa_u32(at, r);
-          st_cluster_b32x2(to, tc::pack_half2(hi[0], hi[1]), tc::pack_half2(hi[2], hi[3]));
-          if constexpr (kSplit) st_cluster_b32x2(to + S * LD * 2, tc::pack_half2(lo[0], lo[1]), tc::pack_half2(lo[2], lo[3]));
+          st_cluster_b32x2(to, hi[0], hi[1]);
+          if constexpr (kSplit) st_cluster_b32x2(to + S * LD * 2, lo[0], lo[1]);
         }
     }
     __syncwarp();
@@ -244,15 +244,22 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = blk / (S / 16) * 16 + g + (i >> 1) * 8, c = blk % (S / 16) * 16 + 8 * t + t2 + (i & 1);
-          float av = __half2float(A[r * LD + c]);
-          if constexpr (kSplit) av += __half2float(A[S * LD + r * LD + c]);
-          const float v = fmaf(q.c * (kB / (kA * kA)), bv[u][t][i], q.b * (kB / kA) * av) + (r == c ? q.a * kB : 0.f);
-          __half hi, lo;
-          tc::split_half(v, hi, lo);
-          B[r * LD + c] = hi;
-          if constexpr (kSplit) B[S * LD + r * LD + c] = lo;
+        for (int h = 0; h < 2; ++h) {
+          const int r = blk / (S / 16) * 16 + g + 8 * h, c = blk % (S / 16) * 16 + 8 * t + t2, at = r * LD + c;
+          float a0, a1;
+          tc::half2_floats(*reinterpret_cast<const uint32_t*>(A + at), a0, a1);
+          if constexpr (kSplit) {
+            float l0, l1;
+            tc::half2_floats(*reinterpret_cast<const uint32_t*>(A + S * LD + at), l0, l1);
+            a0 += l0;
+            a1 += l1;
+          }
+          const float fa = q.b * (kB / kA), fc = q.c * (kB / (kA * kA));
+          uint32_t hi, lo;
+          tc::split_f16x2(fmaf(fc, bv[u][t][2 * h], fa * a0) + (r == c ? q.a * kB : 0.f),
+                          fmaf(fc, bv[u][t][2 * h + 1], fa * a1) + (r == c + 1 ? q.a * kB : 0.f), hi, lo);
+          *reinterpret_cast<uint32_t*>(B + at) = hi;
+          if constexpr (kSplit) *reinterpret_cast<uint32_t*>(B + S * LD + at) = lo;
         }
     }
     __syncthreads();
@@ -286,11 +293,10 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
           const int i = m0 + g + 8 * h, j = n0 + t2;
           const float v[2] = {(hi_acc[2 * h] + lo_acc[2 * h]) * (1.f / kB), (hi_acc[2 * h + 1] + lo_acc[2 * h + 1]) * (1.f / kB)};
           if (!last) {
-            __half hi0, lo0, hi1, lo1;
-            tc::split_half(v[0], hi0, lo0);
-            tc::split_half(v[1], hi1, lo1);
-            *reinterpret_cast<uint32_t*>(X + i * ldx + j) = tc::pack_half2(hi0, hi1);
-            *reinterpret_cast<uint32_t*>(X + xpl + i * ldx + j) = tc::pack_half2(lo0, lo1);
+            uint32_t hi, lo;
+            tc::split_f16x2(v[0], v[1], hi, lo);
+            *reinterpret_cast<uint32_t*>(X + i * ldx + j) = hi;
+            *reinterpret_cast<uint32_t*>(X + xpl + i * ldx + j) = lo;
           } else if (i < q.s) {
 #pragma unroll
             for (int d = 0; d < 2; ++d) {

@@ -119,7 +119,8 @@ def ce_check(got, ref, dtype, D, V, T):
 # one row, one feature, two classes; the edges of 32-column groups, 64-wide K blocks, 128 and 256 tiles from both sides; odd
 # feature counts (rows off the 16 bytes that a copy needs); more tiles than SMs
 CE_SIZES = [(1, 1, 2), (1, 8, 1), (3, 5, 7), (2, 16, 33), (31, 64, 127), (33, 65, 129), (64, 512, 1000), (127, 63, 255),
-            (129, 72, 257), (257, 200, 513), (300, 1000, 2049), (1, 640, 20011), (700, 33, 1111), (513, 264, 5003)]
+            (129, 72, 257), (257, 200, 513), (300, 1000, 2049), (1, 640, 20011), (700, 33, 1111), (513, 264, 5003),
+            (2, 40, 3001), (3, 130, 777), (4, 2048, 1001), (5, 128, 4000), (2, 30000, 50), (65, 96, 300), (2, 77, 3)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
