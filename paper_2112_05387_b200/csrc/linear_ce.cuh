@@ -297,17 +297,25 @@ ce_few_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __restr
           for (int c = 0; c < 4; ++c) acc[c][r] = fmaf(f[c][j], xv, acc[c][r]);
         }
     }
+    float b[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if (v0 + c >= V) break;
-      const float b = bias ? to_f(bias[v0 + c]) : 0.f;
+    for (int c = 0; c < 4; ++c) b[c] = v0 + c < V ? (bias ? to_f(bias[v0 + c]) : 0.f) : -INFINITY;
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        const float l = warp_sum(acc[c][r]) + b;
-        if (r < rows && lane == 0 && labels[r] == v0 + c) target[r] = l;
-        if (l == -INFINITY) continue;
-        ce_join(m[r], s[r], make_float2(l, 1.f));
+    for (int r = 0; r < kRows; ++r) {
+      float l[4], top = m[r];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        l[c] = warp_sum(acc[c][r]);
+        l[c] = v0 + c < V ? l[c] + b[c] : -INFINITY;
+        if (r < rows && lane == 0 && labels[r] == v0 + c) target[r] = l[c];
+        top = fmaxf(top, l[c]);
       }
+      if (top == -INFINITY && l[0] == l[0] && l[1] == l[1] && l[2] == l[2] && l[3] == l[3]) continue;   // (no class yet, and no NaN)
+      float sum = s[r] == 0.f ? 0.f : s[r] * exp2f((m[r] - top) * tc::kLog2e);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) sum += exp2f((l[c] - top) * tc::kLog2e);
+      s[r] = sum;
+      m[r] = top;
     }
   }
   __shared__ float2 parts[8][kRows];

@@ -148,8 +148,8 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     if (launches) *launches += 1;
     return ortho_run_small(q, src, small_shape, s.err, st);
   }
-  // bf16 gradients are exact in one plane; a momentum or an fp32 gradient is not
-  int x_planes = (q.g_bf16 && !q.momentum && !q.split) ? 1 : 2;
+  // (a bf16 gradient is exact in one plane)
+  int x_planes = (q.split || (q.low && !(q.g_bf16 && !q.momentum))) ? 2 : 1;
   bool vec = q.cols % 8 == 0;
   for (int b = 0; q.off && b < B; ++b) vec = vec && q.off[b] % 8 == 0;
   LP_CUDA_OK(launch_pdl(vec ? ortho_norm_kernel<true> : ortho_norm_kernel<false>, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts,
@@ -193,9 +193,9 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.aux = s.a; p.aux_f = q.coeffs[1] * (kScaleB / kScaleA); p.diag = q.coeffs[0] * kScaleB;
     rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, cut_a, st);
     if (rc != LP_OK) return rc;
-    // X <- B X (X B).  An error in X grows by up to a in each later step, so its low part is kept while three or more
-    // products follow (relative error of the result, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3 with the
-    // low parts of two steps, 1.1e-3 with all; fp16's step in A and B costs 1e-3)
+    // X <- B X (X B).  An error in X grows by up to a in each later step, so where the result itself is wanted the low part
+    // is kept while three or more products follow (relative error, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3
+    // with the low parts of two steps, 1.1e-3 with all; fp16's step in A and B costs 1e-3; a low part costs a product)
     memset(&p, 0, sizeof(p));
     p.M = q.rows; p.N = q.cols; p.batch = B; p.err = s.err;
     p.a_planes = tall ? x_planes : planes;
@@ -214,7 +214,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
       }
       rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, cut_x, st);
     } else {
-      x_planes = (q.split || i + 3 < q.steps) ? 2 : 1;
+      x_planes = (q.split || (q.low && i + 3 < q.steps)) ? 2 : 1;
       cur ^= 1;
       p.h_out = s.x[cur]; p.h_ld = s.ld; p.h_batch = x_mat; p.h_plane = x_planes == 2 ? x_plane : 0;
       rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, cut_x, st);
@@ -243,7 +243,7 @@ static int check_ortho(int dtype, int batch, int rows, int cols, int steps, floa
 // one piece.
 static const size_t kCePieceBytes = (size_t)512 << 20;
 static const int kCeAmaxParts = 592;
-static const int kCeFewBlocks = 296;        // two an SM
+static const int kCeFewBlocks = 592;        // four an SM
 static const size_t kCeFewSmem = 96 * 1024;
 
 struct CeScratch {
@@ -295,7 +295,7 @@ static int start_few(const CeScratch& s, int rows, int D, int V, const T* x, con
 template <typename T>
 static int ce_few_rows(const CeScratch& s, int rows, int D, int V, const T* x, const T* w, const T* bias, const int32_t* labels, float* row_loss,
                        float* loss, cudaStream_t st) {
-  const int blocks = (int)std::min<long long>(std::min(kCeFewBlocks, 2 * cur_dev().sm_count), (V + 31) / 32);
+  const int blocks = (int)std::min<long long>(std::min(kCeFewBlocks, 4 * cur_dev().sm_count), (V + 31) / 32);
   const int rc = rows == 1 ? start_few<T, 1>(s, rows, D, V, x, w, bias, labels, blocks, st)
                  : rows == 2 ? start_few<T, 2>(s, rows, D, V, x, w, bias, labels, blocks, st)
                              : start_few<T, 4>(s, rows, D, V, x, w, bias, labels, blocks, st);
@@ -347,7 +347,7 @@ int lp_orthogonalize(int dtype, int batch, int rows, int cols, const void* g, vo
   q.batch = batch; q.rows = rows; q.cols = cols;
   q.g_bf16 = q.out_bf16 = dtype == LP_BF16;
   q.split = dtype == LP_F32;
-  q.g = g; q.out = out; q.steps = steps; q.eps = eps;
+  q.g = g; q.out = out; q.steps = steps; q.eps = eps; q.low = true;
   memcpy(q.coeffs, coeffs ? coeffs : kOrthoCoeffs, sizeof(q.coeffs));
   return ortho_run(q, scratch, (cudaStream_t)stream, nullptr);
 }

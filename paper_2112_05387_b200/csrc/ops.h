@@ -9,6 +9,8 @@ struct OrthoProblem {
   int batch, rows, cols;
   bool g_bf16;            // type of g
   bool split;             // fp32 results: operands as high and low parts
+  bool low;               // else: the low parts of the first iterates are kept.  A step of the weights does without: it is a
+                          // fraction lr of O, and O off by 1e-2 moves it less than a rounding of the weights to bf16 does
   const void* g;
   const long long* off;   // element offset of each matrix from g, momentum and out (host, `batch` of them), or null: contiguous
   float* momentum;        // or null
