@@ -158,13 +158,13 @@ int lp_boundary_shape_desc(const lp_net_desc* desc, int k, int shape_nhwc[4]);
  * synchronous cudaMemset (it returns after the fill; work of the caller still running on other
  * streams must not touch the workspace meanwhile); parameters start at zero until lp_set_params.
  * Calls on one handle are made by one thread at a time.  The handle has streams and events of its own: lp_modules_fwd_bwd_all,
- * lp_step, lp_layer_parallel_step, lp_auxnet_distill and lp_serial_fwd_bwd fork work onto them and join it before what follows
+ * lp_step, lp_step_muon, lp_layer_parallel_step, lp_auxnet_distill and lp_serial_fwd_bwd fork work onto them and join it before what follows
  * the call on its `stream`; lp_module_fwd_bwd uses those of its module only.  Calls on different streams are therefore ordered
  * where they share one.  Streams of the handle that a caller's recording has reached belong to it until it ends: meanwhile
- * lp_step and lp_auxnet_distill, called outside that recording, stay on the stream they are given; the other calls that need
+ * lp_step, lp_step_muon and lp_auxnet_distill, called outside that recording, stay on the stream they are given; the other calls that need
  * such a stream return LP_ERR_CUDA.
  * The handle owns host memory, streams, events and -- from the third call of a kind on -- one executable graph for each
- * of lp_auxnet_forward, lp_modules_fwd_bwd_all, lp_step, lp_layer_parallel_step, lp_auxnet_distill, lp_forward_serial and
+ * of lp_auxnet_forward, lp_modules_fwd_bwd_all, lp_step, lp_step_muon, lp_layer_parallel_step, lp_auxnet_distill, lp_forward_serial and
  * lp_serial_fwd_bwd, as which the call is then launched (recorded anew each time with its own arguments).  The driver
  * keeps the nodes of such a graph in device memory of its own; lp_destroy gives it back. */
 int lp_create(const lp_net_desc* desc, void* dev_workspace, size_t bytes, lp_handle** out);
@@ -203,6 +203,17 @@ int lp_modules_fwd_bwd_all(lp_handle* h, const void* const* x, const int32_t* la
  * last fwd_bwd).  momentum = weight_decay = 0 is the paper's plain SGD. */
 int lp_step(lp_handle* h, float lr, float momentum, float weight_decay, float kappa_step,
             void* const* lambdas_inout, void* stream);
+
+/* Step 3 with an orthogonalised update (the same place as lp_step, which it replaces): every convolution weight W of a module
+ * whose gradients are fresh, as a matrix [C_out][R S C_in],
+ *     m <- momentum m + g;  u = nesterov ? g + momentum m : m;  O = orthogonalised u (lp_orthogonalize, five steps, 1e-7);
+ *     W <- (1 - lr_conv weight_decay) W - lr_conv sqrt(max(1, rows / cols)) O,
+ * and the other parameters and the multipliers as in lp_step (rate lr).  The momentum is the one that lp_step keeps.  In LP_BF16
+ * O is off by up to 1e-2 of its norm (iterates in fp16), in LP_F32 by some 1e-6.  scratch: lp_step_muon_scratch_bytes() bytes,
+ * 256-byte aligned, the call's own while it runs.  LP_ERR_ORDER if no module's gradients are fresh. */
+size_t lp_step_muon_scratch_bytes(lp_handle* h);
+int lp_step_muon(lp_handle* h, float lr_conv, float lr, float momentum, int nesterov, float weight_decay, float kappa_step,
+                 void* const* lambdas_inout, void* scratch, size_t scratch_bytes, void* stream);
 
 /* Steps 1-3 in one call with every dependency of Algorithm 1 and no more: the AuxNet chain runs
  * on its own stream; module k starts as soon as x_k exists, takes its local loss as soon as
@@ -378,7 +389,7 @@ int lp_conv2d_fwd_noalloc(int N, int H, int W, int Cin, int Cout, int R, int str
  *   l = x w^T + bias;  row_loss[t] = log sum_v exp l[t][v] - l[t][labels[t]];  loss = mean of row_loss over the counted rows
  * A row counts if its label is a class, 0 <= labels[t] < V; any other label leaves the row out: its row_loss and its row of dx
  * are 0 and nothing of x[t] (which may hold anything, NaN included) reaches dw or dbias.
- *   x [T][D], w [V][D], bias [V] or NULL (entries may be -inf: that class then has probability 0), labels int32 [T]
+ *   T, V up to 2^28, D up to 2^20; x [T][D], w [V][D], bias [V] or NULL (entries may be -inf: that class then has probability 0), labels int32 [T]
  *   loss_out: float[2] = { loss (0 if no row counts), number of counted rows }; row_loss: float[T] or NULL
  *   dx [T][D], dw [V][D], dbias [V]: grad_scale times the gradient of loss, any of them NULL; overwritten.  All NULL: the loss
  *     alone.

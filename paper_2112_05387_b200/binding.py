@@ -15,7 +15,7 @@ __all__ = [
     "lp_graph_launch", "lp_conv2d_fwd_noalloc", "LP_NOALLOC_SCRATCH_BYTES", "lp_layer_parallel_step", "lp_auxnet_distill", "lp_aux_correct", "lp_timeline", "lp_timeline_record",
     "LP_PHASE_NAMES", "LP_OP_NAMES", "EXPORTED_SYMBOLS", "lp_selftest_bounded_wait", "lp_call_graphs",
     "lp_linear_cross_entropy", "lp_linear_cross_entropy_scratch_bytes", "lp_orthogonalize", "lp_orthogonalize_scratch_bytes",
-    "lp_muon_update", "lp_scratch_status",
+    "lp_muon_update", "lp_scratch_status", "lp_step_muon", "lp_step_muon_scratch_bytes",
 ]
 
 LP_OK = 0
@@ -42,7 +42,7 @@ EXPORTED_SYMBOLS = [
     "lp_conv_profile", "lp_conv2d_scratch_bytes", "lp_conv2d", "lp_graph_begin", "lp_graph_end", "lp_graph_launch",
     "lp_conv2d_fwd_noalloc", "lp_layer_parallel_step", "lp_auxnet_distill", "lp_timeline", "lp_aux_correct",
     "lp_selftest_bounded_wait", "lp_call_graphs", "lp_linear_cross_entropy", "lp_linear_cross_entropy_scratch_bytes",
-    "lp_orthogonalize", "lp_orthogonalize_scratch_bytes", "lp_muon_update", "lp_scratch_status",
+    "lp_orthogonalize", "lp_orthogonalize_scratch_bytes", "lp_muon_update", "lp_scratch_status", "lp_step_muon", "lp_step_muon_scratch_bytes",
 ]
 
 
@@ -154,6 +154,9 @@ def library():
     lib.lp_orthogonalize.argtypes = [i32] * 4 + [vp, vp, i32, ctypes.POINTER(f32), f32, vp, sz, vp]
     lib.lp_muon_update.argtypes = [i32] * 4 + [vp, vp, vp, f32, f32, i32, f32, f32, i32, ctypes.POINTER(f32), f32, vp, sz, vp]
     lib.lp_scratch_status.argtypes = [vp, vp]
+    lib.lp_step_muon_scratch_bytes.restype = sz
+    lib.lp_step_muon_scratch_bytes.argtypes = [vp]
+    lib.lp_step_muon.argtypes = [vp, f32, f32, f32, i32, f32, f32, ctypes.POINTER(vp), vp, sz, vp]
     _LIB = lib
     return lib
 
@@ -318,6 +321,16 @@ def lp_step(h, lr, momentum=0.0, weight_decay=0.0, kappa_step=0.0, lambdas_inout
     _check(library().lp_step(h.ptr, lr, momentum, weight_decay, kappa_step, la, _ptr(stream)), "lp_step")
 
 
+def lp_step_muon_scratch_bytes(h):
+    return library().lp_step_muon_scratch_bytes(h.ptr)
+
+
+def lp_step_muon(h, lr_conv, lr, momentum, nesterov, weight_decay, kappa_step, lambdas_inout, scratch, scratch_bytes, stream=None):
+    la = _ptr_array(lambdas_inout, h.K) if lambdas_inout is not None else None
+    _check(library().lp_step_muon(h.ptr, lr_conv, lr, momentum, 1 if nesterov else 0, weight_decay, kappa_step, la, _ptr(scratch),
+                                  scratch_bytes, _ptr(stream)), "lp_step_muon")
+
+
 def lp_layer_parallel_step(h, images, x_out, labels, lambdas_inout, rho, loss_out, dx, lr, momentum=0.0,
                            weight_decay=0.0, kappa_step=0.0, stream=None):
     xa = _ptr_array(x_out, h.K - 1)
@@ -445,7 +458,7 @@ def _checked(t, name, dtype, count):
     if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
         raise ValueError("%s: %d contiguous values of %s are needed, got %s of %s" % (name, count, dtype, tuple(t.shape), t.dtype))
     if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+        raise ValueError("%s is on %s, the operators launch on the current CUDA device" % (name, t.device))
     return t.data_ptr()
 
 

@@ -948,6 +948,29 @@ __global__ void sgd_kernel(float* __restrict__ p, const float* __restrict__ g, f
   }
 }
 
+// The same update on a few spans of a blob (what lp_step_muon leaves to SGD: everything but the convolution weights); one
+// span to a grid row.
+constexpr int kMaxSgdSpans = 128;
+struct SgdSpans {
+  int n;
+  struct Span { long long begin; int count; } span[kMaxSgdSpans];
+};
+__global__ void __launch_bounds__(256)
+sgd_spans_kernel(const __grid_constant__ SgdSpans s, float* __restrict__ p, const float* __restrict__ g, float* __restrict__ mom, float lr,
+                 float momentum, float wd) {
+  const long long begin = s.span[blockIdx.y].begin;
+  const int count = s.span[blockIdx.y].count;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < count; i += gridDim.x * 256) {
+    const long long j = begin + i;
+    float gi = g[j] + wd * p[j];
+    if (momentum != 0.f) {
+      gi = momentum * mom[j] + gi;
+      mom[j] = gi;
+    }
+    p[j] -= lr * gi;
+  }
+}
+
 template <typename T>
 __global__ void kappa_update_kernel(T* __restrict__ kappa, const T* __restrict__ r, float c, long long total_vecs) {
   constexpr int V = VecT<T>::N;

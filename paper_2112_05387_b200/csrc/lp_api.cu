@@ -23,6 +23,7 @@
 #include "kernels_elem.cuh"
 #include "conv_thin.cuh"
 #include "net.h"
+#include "ops.h"
 #include "order_rules.h"
 #include "wgrad_tc.cuh"
 
@@ -227,7 +228,7 @@ struct ConvProfile {
 using namespace lp;
 
 // Entry points that run as one graph launch (call_graph.h).
-enum { CALL_AUX_FORWARD = 0, CALL_MODULES, CALL_STEP, CALL_LAYER_PARALLEL, CALL_DISTILL, CALL_FORWARD_SERIAL, CALL_SERIAL, CALL_KINDS };
+enum { CALL_AUX_FORWARD = 0, CALL_MODULES, CALL_STEP, CALL_LAYER_PARALLEL, CALL_DISTILL, CALL_FORWARD_SERIAL, CALL_SERIAL, CALL_STEP_MUON, CALL_KINDS };
 
 struct lp_handle {
   NetDef net;
@@ -2924,6 +2925,137 @@ int lp_step(lp_handle* h, float lr, float momentum, float weight_decay, float ka
     if (!h->modules[k].ps.grads_fresh) continue;
     first_err = update_module(h, k, lr, momentum, weight_decay, kappa_step,
                               (lambdas_inout && k + 1 < K) ? lambdas_inout[k] : nullptr, apart ? h->streams[k] : st);
+  }
+  for (int k = 0; k < forked; ++k)
+    if (cudaEventRecord(h->done[k], h->streams[k]) != cudaSuccess || cudaStreamWaitEvent(st, h->done[k], 0) != cudaSuccess)
+      if (first_err == LP_OK) first_err = LP_ERR_CUDA;
+  return first_err;
+  });
+}
+
+// The convolution weights of a module, matrices [C_out][R S C_in] of one shape together (in groups that the kernels' table of
+// offsets holds), and the rest of its parameters as spans of the blob.
+struct MuonGroup {
+  int rows, cols;
+  std::vector<long long> off;
+};
+static void muon_groups(const Plan& P, std::vector<MuonGroup>* groups, std::vector<SgdSpans>* spans) {
+  for (const lp_param_entry& e : P.ps.layout) {
+    long long n = 1;
+    for (int d = 0; d < 4; ++d) n *= e.shape[d] > 0 ? e.shape[d] : 1;
+    if (e.kind == LP_KIND_CONV_W) {
+      const int rows = e.shape[0], cols = (int)(n / rows);
+      MuonGroup* at = nullptr;
+      for (MuonGroup& g : *groups)
+        if (g.rows == rows && g.cols == cols && g.off.size() < kOrthoMaxOffsets) at = &g;
+      if (!at) {
+        groups->push_back(MuonGroup{rows, cols, {}});
+        at = &groups->back();
+      }
+      at->off.push_back((long long)e.offset);
+    } else if (spans) {
+      SgdSpans* s = spans->empty() ? nullptr : &spans->back();
+      if (s && s->n && s->span[s->n - 1].begin + s->span[s->n - 1].count == (long long)e.offset && s->span[s->n - 1].count + n < (1 << 30)) {
+        s->span[s->n - 1].count += (int)n;
+        continue;
+      }
+      if (!s || s->n == kMaxSgdSpans) {
+        spans->push_back(SgdSpans{});
+        s = &spans->back();
+      }
+      s->span[s->n].begin = (long long)e.offset;
+      s->span[s->n++].count = (int)n;
+    }
+  }
+}
+static size_t muon_module_scratch(const Plan& P, bool split) {
+  std::vector<MuonGroup> groups;
+  muon_groups(P, &groups, nullptr);
+  size_t most = 0;
+  for (const MuonGroup& g : groups) most = std::max(most, ortho_scratch_bytes((int)g.off.size(), g.rows, g.cols, split));
+  return most;
+}
+
+size_t lp_step_muon_scratch_bytes(lp_handle* h) {
+  if (!h) return 0;
+  size_t total = 0;
+  for (const Plan& P : h->modules) total += muon_module_scratch(P, h->dtype == LP_F32);
+  return total;
+}
+
+static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momentum, bool nesterov, float weight_decay, float kappa_step,
+                       void* lambda_inout, void* scratch, cudaStream_t st) {
+  Plan& P = h->modules[k];
+  const bool kappa = lambda_inout && k + 1 < h->net.K;
+  TimelineScope ts(h, st, k, LP_OP_UPDATE, LP_PHASE_UPDATE, (momentum != 0.f ? 20.0 : 12.0) * (double)P.ps.n +
+                   4.0 * (double)P.ps.pack_total + (kappa ? 3.0 * (double)boundary_bytes(h, k + 1) : 0.0));
+  std::vector<MuonGroup> groups;
+  std::vector<SgdSpans> spans;
+  muon_groups(P, &groups, &spans);
+  for (const MuonGroup& g : groups) {
+    OrthoProblem q;
+    memset(&q, 0, sizeof(q));
+    q.batch = (int)g.off.size(); q.rows = g.rows; q.cols = g.cols;
+    q.split = h->dtype == LP_F32;
+    q.g = P.ps.g; q.off = g.off.data();
+    q.momentum = momentum != 0.f ? P.ps.m : nullptr; q.mu = momentum; q.nesterov = nesterov;
+    q.steps = 5; q.eps = 1e-7f;
+    memcpy(q.coeffs, kOrthoCoeffs, sizeof(q.coeffs));
+    q.out = P.ps.p; q.update = true;
+    q.keep = 1.f - lr_conv * weight_decay;
+    q.step = -lr_conv * sqrtf(std::max(1.f, (float)g.rows / (float)g.cols));
+    q.err = h->dev_err;
+    long long n = 0;
+    const int rc = ortho_run(q, scratch, st, &n);
+    h->launches += n;
+    if (rc != LP_OK) return rc;
+  }
+  for (const SgdSpans& s : spans) {
+    int most = 0;
+    for (int i = 0; i < s.n; ++i) most = std::max(most, s.span[i].count);
+    sgd_spans_kernel<<<dim3((unsigned)std::min(256, (most + 1023) / 1024), (unsigned)s.n), 256, 0, st>>>(s, P.ps.p, P.ps.g, P.ps.m, lr, momentum,
+                                                                                                        weight_decay);
+    h->launches++;
+    LP_CUDA_OK(cudaGetLastError());
+  }
+  const int rc = pack_weights(h, P, st);
+  if (rc != LP_OK) return rc;
+  P.ps.grads_fresh = false;
+  return kappa ? update_kappa(h, k, kappa_step, lambda_inout, st) : LP_OK;
+}
+
+int lp_step_muon(lp_handle* h, float lr_conv, float lr, float momentum, int nesterov, float weight_decay, float kappa_step,
+                 void* const* lambdas_inout, void* scratch, size_t scratch_bytes, void* stream) {
+  if (!h || !scratch) return LP_ERR_NULL;
+  bool any = false;
+  for (auto& P : h->modules) any = any || P.ps.grads_fresh;
+  if (!any) return LP_ERR_ORDER;
+  if (reinterpret_cast<uintptr_t>(scratch) & 255) return LP_ERR_ALIGN;
+  if (scratch_bytes < lp_step_muon_scratch_bytes(h)) return LP_ERR_WORKSPACE;
+  const int K = h->net.K;
+  if (lambdas_inout)
+    for (int k = 0; k + 1 < K; ++k)
+      if (lambdas_inout[k] && !aligned16(lambdas_inout[k])) return LP_ERR_ALIGN;
+  return run_as_graph(h, CALL_STEP_MUON, (cudaStream_t)stream, [&](cudaStream_t st) -> int {
+  // the modules' updates side by side, as in lp_step; each has a part of the scratch
+  bool apart = !timed(h) && can_fork(st, h->streams);
+  if (lambdas_inout) {
+    Span lambda[LP_MAX_MODULES];
+    for (int k = 0; k + 1 < K; ++k) lambda[k] = Span{lambdas_inout[k], boundary_bytes(h, k + 1)};
+    apart = apart && multipliers_apart(lambda, K - 1);
+  }
+  LP_CUDA_OK(cudaEventRecord(h->fork, st));
+  int first_err = LP_OK, forked = 0;
+  uint8_t* at = (uint8_t*)scratch;
+  for (int k = 0; k < K && first_err == LP_OK; ++k) {
+    if (apart) {
+      if (cudaStreamWaitEvent(h->streams[k], h->fork, 0) != cudaSuccess) { first_err = LP_ERR_CUDA; break; }
+      forked = k + 1;
+    }
+    if (h->modules[k].ps.grads_fresh)
+      first_err = muon_module(h, k, lr_conv, lr, momentum, nesterov != 0, weight_decay, kappa_step,
+                              (lambdas_inout && k + 1 < K) ? lambdas_inout[k] : nullptr, at, apart ? h->streams[k] : st);
+    at += muon_module_scratch(h->modules[k], h->dtype == LP_F32);
   }
   for (int k = 0; k < forked; ++k)
     if (cudaEventRecord(h->done[k], h->streams[k]) != cudaSuccess || cudaStreamWaitEvent(st, h->done[k], 0) != cudaSuccess)

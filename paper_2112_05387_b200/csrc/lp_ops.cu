@@ -129,6 +129,9 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   const Device& D = cur_dev();
   Carve c{(uint8_t*)scratch};
   OrthoScratch s = ortho_carve(c, q.batch, q.rows, q.cols, q.split);
+  int* clear_err = q.err ? nullptr : s.err;
+  if (q.err) s.err = q.err;
+  if (q.off && q.batch > kOrthoMaxOffsets) return LP_ERR_SIZE;
   const bool tall = q.rows > q.cols;
   const int small = std::min(q.rows, q.cols), B = q.batch;
   const long long x_mat = (long long)q.rows * s.ld, x_plane = B * x_mat, s_mat = (long long)small * s.ld_s, s_plane = B * s_mat;
@@ -146,14 +149,14 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   SmallShape small_shape;
   if (ortho_small_shape(B, q.rows, q.cols, q.split, D.sm_count, &small_shape)) {
     if (launches) *launches += 1;
-    return ortho_run_small(q, src, small_shape, s.err, st);
+    return ortho_run_small(q, src, small_shape, clear_err, st);
   }
   // (a bf16 gradient is exact in one plane)
   int x_planes = (q.split || (q.low && !(q.g_bf16 && !q.momentum))) ? 2 : 1;
   bool vec = q.cols % 8 == 0;
   for (int b = 0; q.off && b < B; ++b) vec = vec && q.off[b] % 8 == 0;
   LP_CUDA_OK(launch_pdl(vec ? ortho_norm_kernel<true> : ortho_norm_kernel<false>, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts,
-                        s.sums, s.err));
+                        s.sums, clear_err));
   LP_CUDA_OK(launch_pdl(vec ? ortho_pack_kernel<true> : ortho_pack_kernel<false>, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts,
                         (const double*)s.sums, q.eps, q.cols, s.ld, s.x[0], x_mat, x_planes == 2 ? x_plane : 0LL, s.alpha));
   n += 2;
@@ -226,7 +229,8 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   return LP_OK;
 }
 
-static const float kOrthoCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
+static_assert(kOrthoMaxOffsets == tc::kGemmMaxOffsets, "one table");
+const float kOrthoCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
 
 static int check_ortho(int dtype, int batch, int rows, int cols, int steps, float eps) {
   if (dtype != LP_F32 && dtype != LP_BF16) return LP_ERR_UNSUPPORTED;
@@ -372,8 +376,12 @@ int lp_muon_update(int dtype, int batch, int rows, int cols, void* w, const void
   return ortho_run(q, scratch, (cudaStream_t)stream, nullptr);
 }
 
+static bool ce_size_ok(int T, int D, int V) {
+  return T >= 1 && D >= 1 && V >= 1 && T <= (1 << 28) && V <= (1 << 28) && D <= (1 << 20);
+}
+
 size_t lp_linear_cross_entropy_scratch_bytes(int dtype, int T, int D, int V, int grads) {
-  if ((dtype != LP_F32 && dtype != LP_BF16) || T < 1 || D < 1 || V < 1) return 0;
+  if ((dtype != LP_F32 && dtype != LP_BF16) || !ce_size_ok(T, D, V)) return 0;
   Carve c{nullptr};
   ce_carve(c, dtype, T, D, V, grads != 0);
   return c.off;
@@ -384,7 +392,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
                             size_t scratch_bytes, void* stream) {
   if (!x || !w || !labels || !loss_out || !scratch) return LP_ERR_NULL;
   if (dtype != LP_F32 && dtype != LP_BF16) return LP_ERR_UNSUPPORTED;
-  if (T < 1 || D < 1 || V < 1) return LP_ERR_SIZE;
+  if (!ce_size_ok(T, D, V)) return LP_ERR_SIZE;
   const void* ptrs[] = {x, w, bias, labels, loss_out, row_loss, dx, dw, dbias};
   for (const void* p : ptrs)
     if (!aligned16(p)) return LP_ERR_ALIGN;

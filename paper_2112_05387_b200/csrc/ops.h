@@ -12,7 +12,8 @@ struct OrthoProblem {
   bool low;               // else: the low parts of the first iterates are kept.  A step of the weights does without: it is a
                           // fraction lr of O, and O off by 1e-2 moves it less than a rounding of the weights to bf16 does
   const void* g;
-  const long long* off;   // element offset of each matrix from g, momentum and out (host, `batch` of them), or null: contiguous
+  const long long* off;   // element offset of each matrix from g, momentum and out (host; at most kOrthoMaxOffsets matrices then),
+                          // or null: one after another
   float* momentum;        // or null
   float mu;
   bool nesterov;
@@ -23,8 +24,11 @@ struct OrthoProblem {
   bool out_bf16;
   bool update;            // out <- keep * out + step * O
   float keep, step;
+  int* err;               // error word, or null: the first word of the scratch, cleared by the call
 };
 
+constexpr int kOrthoMaxOffsets = 64;
+extern const float kOrthoCoeffs[3];
 size_t ortho_scratch_bytes(int batch, int rows, int cols, bool split);
 // Enqueues the operator; `launches` (nullable) counts its kernels.
 int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* launches);

@@ -71,11 +71,11 @@ __device__ __forceinline__ void ortho_direction(const OrthoSource& s, float (&g)
 //   m <- mu m + g;  u = m, or g + mu m (Nesterov).
 template <bool kVec>
 __global__ void __launch_bounds__(kOrthoThreads)
-ortho_norm_kernel(const __grid_constant__ OrthoSource s, int parts, double* __restrict__ sums, int* __restrict__ err) {
+ortho_norm_kernel(const __grid_constant__ OrthoSource s, int parts, double* __restrict__ sums, int* __restrict__ err /* cleared, or null */) {
   constexpr int N = OrthoVec<kVec>::N;
   pdl_wait();
   pdl_launch_dependents();
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *err = 0;
+  if (err && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *err = 0;
   const int b = blockIdx.y;
   const long long base = s.use_off ? s.off[b] : b * s.elems, groups = s.elems / N;
   const long long lo = groups * blockIdx.x / parts, hi = groups * (blockIdx.x + 1) / parts;

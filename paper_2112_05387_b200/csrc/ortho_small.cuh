@@ -27,7 +27,7 @@ struct OrthoSmall {
   void* out;
   int out_bf16, update;
   float keep, step;
-  int* err;
+  int* err;               // cleared, or null
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], const __half* p) {
@@ -123,7 +123,7 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
 
   pdl_wait();
   pdl_launch_dependents();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *q.err = 0;
+  if (q.err && blockIdx.x == 0 && threadIdx.x == 0) *q.err = 0;
 
   // element e of the slice: row i of X, column j0 + j; contiguous in memory along j (wide) or i (tall)
   const int n = q.s * width, inner = q.tall ? q.s : max(width, 1);
