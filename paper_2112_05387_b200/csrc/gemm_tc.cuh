@@ -58,6 +58,9 @@ struct GemmParams {
   int round_len;                  // kRounds: K blocks per accumulation
   int a_mn, b_mn;                 // 1: the operand's row index is the contiguous one
   uint32_t idesc;
+  // 1: the kernel before reads and writes nothing of this one's (and has itself waited for what this one reads, before it let
+  // this one start): the two run side by side, and this one waits for that one's end before its own
+  int wait_late;
   int* err;
   // scale of the accumulator: f * f_dev[b]^f_pow
   float f;
@@ -401,10 +404,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   __syncthreads();
   if constexpr (kCluster) cluster_sync_all();   // both CTAs' barriers exist before anything signals them from the other side
   tc_fence_after();
-  pdl_wait();
+  if (!p.wait_late) pdl_wait();
   pdl_launch_dependents();
   const uint32_t tmem_base = tail->tmem_base;
-  // (its share of K: at least one K block, see gemm_kind)
+  // (its share of K: at least one K block, see gemm_cut)
   const int k_first = kKSplit ? p.kblocks * (int)crank / ctas : 0;
   const int steps = kKSplit ? p.kblocks * (int)(crank + 1) / ctas - k_first : p.kblocks;
   constexpr bool kRounds = kMode == GEMM_SPLIT;
@@ -681,6 +684,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll 1
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
   }
+  if (p.wait_late) pdl_wait();
   if constexpr (kCluster) cluster_sync_all();   // no CTA leaves while another may still signal it or write its ring
   if (warp == 2) {
     tc_fence_after();

@@ -41,6 +41,20 @@ __device__ __forceinline__ float block_sum(float v, float* part) {
   return s;
 }
 
+// Number of rows that count, by one block; to thread 0.
+__device__ __forceinline__ int ce_count_rows(const int32_t* labels, int T, int V) {
+  int n = 0;
+  for (int t = threadIdx.x; t < T; t += kCeThreads) n += ce_counts(labels[t], V);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+  __shared__ int cnt[kCeThreads / 32];
+  if ((threadIdx.x & 31) == 0) cnt[threadIdx.x >> 5] = n;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    for (int i = 1; i < kCeThreads / 32; ++i) n += cnt[i];
+  return n;
+}
+
 // Block 0 counts the rows; for fp32 problems the others take the largest finite magnitudes of x and w (parts of each).
 __global__ void __launch_bounds__(kCeThreads)
 ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int V, const float* __restrict__ x, long long nx, const float* __restrict__ w,
@@ -49,15 +63,8 @@ ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int V, const float*
   pdl_launch_dependents();
   __shared__ float part[kCeThreads / 32];
   if (blockIdx.x == 0) {
-    int n = 0;
-    for (int t = threadIdx.x; t < T; t += kCeThreads) n += ce_counts(labels[t], V);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-    __shared__ int cnt[kCeThreads / 32];
-    if ((threadIdx.x & 31) == 0) cnt[threadIdx.x >> 5] = n;
-    __syncthreads();
+    const int n = ce_count_rows(labels, T, V);
     if (threadIdx.x == 0) {
-      for (int i = 1; i < kCeThreads / 32; ++i) n += cnt[i];
       hdr->err = 0;
       hdr->count = n;
     }
@@ -94,7 +101,7 @@ __device__ __forceinline__ float ce_scale_of(float amax) {
 
 // The operands as the products take them, rows `ld` apart: fp32 as fp16 high and low parts of the scaled values, bf16 as it is.
 // Rows of x whose label is no class become zeros: what stands there (padding, NaN) must not reach dw through a product with 0.
-// Blocks [0, xb) take x, the rest w (none where it is used in place).  The first block writes the header's scales.  kVec: D is a
+// Blocks [1, xb) take x, the rest w (none where it is used in place), block 0 nothing but the header (bf16 problems: the count of rows with it).  kVec: D is a
 // multiple of 8.
 template <bool kVec>
 __global__ void __launch_bounds__(kCeThreads)
@@ -114,9 +121,14 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int
     if ((threadIdx.x & 31) == 0) scales[which] = is_bf16 ? 1.f : ce_scale_of(m);
   }
   __syncthreads();
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    const int n = hdr->count;
-    const float gf = n > 0 ? g / (float)n : 0.f;
+  if (blockIdx.x == 0) {
+    const int counted = is_bf16 ? ce_count_rows(labels, T, V) : hdr->count;
+    if (threadIdx.x) return;
+    if (is_bf16) {
+      hdr->err = 0;
+      hdr->count = counted;
+    }
+    const float gf = counted > 0 ? g / (float)counted : 0.f;
     const float dl = is_bf16 ? 1.f : 1.f / kCeDlScale;
     hdr->x_scale = scales[0];
     hdr->w_scale = scales[1];
@@ -124,9 +136,10 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int
     hdr->grad_f = gf;
     hdr->dx_f = gf * dl * (1.f / scales[1]);
     hdr->dw_f = gf * dl * (1.f / scales[0]);
+    return;
   }
   const bool of_w = (int)blockIdx.x >= xb;
-  const int blk = of_w ? blockIdx.x - xb : blockIdx.x, blks = of_w ? gridDim.x - xb : xb;
+  const int blk = of_w ? blockIdx.x - xb : blockIdx.x - 1, blks = of_w ? gridDim.x - xb : xb - 1;
   const void* src = of_w ? w : x;
   __half* dst = of_w ? wo : xo;
   const long long plane = of_w ? w_plane : x_plane;

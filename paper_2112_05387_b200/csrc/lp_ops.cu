@@ -153,9 +153,10 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   }
   // (a bf16 gradient is exact in one plane)
   int x_planes = (q.split || (q.low && !(q.g_bf16 && !q.momentum))) ? 2 : 1;
-  bool vec = q.cols % 8 == 0;
-  for (int b = 0; q.off && b < B; ++b) vec = vec && q.off[b] % 8 == 0;
-  LP_CUDA_OK(launch_pdl(vec ? ortho_norm_kernel<true> : ortho_norm_kernel<false>, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts,
+  bool flat = B == 1 || src.elems % 8 == 0 || q.off;   // every matrix starts on a group of 8 elements
+  for (int b = 0; q.off && b < B; ++b) flat = flat && q.off[b] % 8 == 0;
+  const bool vec = flat && q.cols % 8 == 0;
+  LP_CUDA_OK(launch_pdl(flat ? ortho_norm_kernel<true> : ortho_norm_kernel<false>, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts,
                         s.sums, clear_err));
   LP_CUDA_OK(launch_pdl(vec ? ortho_pack_kernel<true> : ortho_pack_kernel<false>, dim3(s.parts, B), dim3(kOrthoThreads), 0, st, src, s.parts,
                         (const double*)s.sums, q.eps, q.cols, s.ld, s.x[0], x_mat, x_planes == 2 ? x_plane : 0LL, s.alpha));
@@ -412,10 +413,11 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     return s.f32 ? ce_few_rows(s, T, D, V, (const float*)x, (const float*)w, (const float*)bias, labels, rl, loss_out, st)
                  : ce_few_rows(s, T, D, V, (const bf16*)x, (const bf16*)w, (const bf16*)bias, labels, rl, loss_out, st);
   const int amax_blocks = s.f32 ? 2 * kCeAmaxParts : 0;
-  LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + amax_blocks), dim3(kCeThreads), 0, st, labels, T, V, (const float*)x, (long long)T * D,
+  if (s.f32 || !s.x)
+    LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + amax_blocks), dim3(kCeThreads), 0, st, labels, T, V, (const float*)x, (long long)T * D,
                         (const float*)w, (long long)V * D, s.amax, kCeAmaxParts, s.hdr));
   if (s.x) {
-    const int xb = grid_for((long long)T * D, kCeThreads * 8, Dv.sm_count, 4);
+    const int xb = 1 + grid_for((long long)T * D, kCeThreads * 8, Dv.sm_count, 4);
     const int wb = s.w ? grid_for((long long)V * D, kCeThreads * 8, Dv.sm_count, 8) : 0;
     LP_CUDA_OK(launch_pdl(D % 8 ? ce_pack_kernel<false> : ce_pack_kernel<true>, dim3(xb + wb), dim3(kCeThreads), 0, st, x, w, labels, is_bf16, T, D, V, s.ld_d, s.x, x_plane, s.w,
                           w_plane, xb, (const float*)s.amax, kCeAmaxParts, grad_scale, s.hdr));
@@ -447,7 +449,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     p.h_out = s.p; p.h_ld = s.ld_v; p.h_plane = s.f32 ? p_plane : 0;
     if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, cut, st)) != LP_OK) return rc;
     // few rows and parts: one block does the rest of the loss
-    finished = rows == T && (long long)rows * parts <= 16384;
+    finished = rows == T && rows <= 64 && parts <= 128;
     if (finished)
       LP_CUDA_OK(launch_pdl(ce_finish_kernel, dim3(1), dim3(1024), 0, st, (const float2*)s.stats, (long long)s.rows, parts, rows, V, labels,
                             (const float*)s.target, s.lse, rl, loss_out));
@@ -462,6 +464,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
                           p_plane, rows, V, (const float2*)s.stats, (long long)s.rows, part_cols, (const float*)(s.lse + r0),
                           (const float*)(s.target + r0), labels + r0, sums, one_slab ? dbias : nullptr, (const CeHeader*)s.hdr));
     slab0 += slabs;
+    bool dx_idle = false;
     const GemmOperand op{s.p, V, rows, s.ld_v, p_plane, planes, !s.f32};
     if (dx) {
       if ((rc = encode_gemm_map(&m_pk, op, false)) != LP_OK) return rc;
@@ -472,6 +475,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
       const GemmCut kd = gemm_cut(rows, D, V, 1, false, planes, planes);
       if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, kd, st)) != LP_OK) return rc;
+      dx_idle = p.total_tiles * kd.ctas < Dv.sm_count;
     }
     if (dw) {
       if ((rc = encode_gemm_map(&m_pm, op, true)) != LP_OK) return rc;
@@ -481,6 +485,9 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.a_planes = p.b_planes = planes;
       p.f = 1.f; p.f_dev = &s.hdr->dw_f; p.f_pow = 1;
       p.out = dw; p.out_bf16 = is_bf16; p.out_ld = D;
+      // (beside dx's product where that leaves SMs idle: 64 rows x 512 x 1000 30 us and 33 one after the other, fp32 43 and 48;
+      // where it has all of them the two share L2 badly, 4096 x 2048 x 32000 1.32 ms and 1.31)
+      p.wait_late = dx_idle;
       if (s.rows < T) {
         p.acc = s.f32 ? (float*)dw : s.acc;
         p.acc_first = r0 == 0;

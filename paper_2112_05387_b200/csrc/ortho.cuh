@@ -29,7 +29,7 @@ struct OrthoSource {
   long long off[tc::kGemmMaxOffsets];
 };
 
-// kVec: eight elements at a time (columns and offsets are multiples of 8), else one.
+// kVec: eight elements at a time (matrices start on a multiple of 8 elements), else one.
 template <bool kVec>
 struct OrthoVec {
   static constexpr int N = kVec ? 8 : 1;
@@ -66,6 +66,26 @@ __device__ __forceinline__ void ortho_direction(const OrthoSource& s, float (&g)
   for (int j = 0; j < N; ++j) g[j] = s.nesterov ? fmaf(s.mu, m[j], g[j]) : m[j];
 }
 
+// Updates the momentum of a group (if there is one); the sum of squares of what is orthogonalised.
+template <bool kVec>
+__device__ __forceinline__ double ortho_square(const OrthoSource& s, long long i) {
+  constexpr int N = OrthoVec<kVec>::N;
+  float u[N];
+  ortho_load<kVec>(s.g, s.g_bf16, i, u);
+  if (s.momentum) {
+    float m[N];
+    ortho_load<kVec>(s.momentum, 0, i, m);
+#pragma unroll
+    for (int j = 0; j < N; ++j) m[j] = fmaf(s.mu, m[j], u[j]);
+    ortho_store<kVec>(s.momentum, i, m);
+    ortho_direction(s, u, m);
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) sum += (double)u[j] * (double)u[j];
+  return sum;
+}
+
 // Sums of squares of what is orthogonalised, `parts` partial sums a matrix, in fp64 (a gradient of 1e-25 or 1e25 squares out of
 // fp32's range); the momentum is updated on the way:
 //   m <- mu m + g;  u = m, or g + mu m (Nesterov).
@@ -81,20 +101,9 @@ ortho_norm_kernel(const __grid_constant__ OrthoSource s, int parts, double* __re
   const long long lo = groups * blockIdx.x / parts, hi = groups * (blockIdx.x + 1) / parts;
   double sum = 0.0;
 #pragma unroll 2
-  for (long long i = lo + threadIdx.x; i < hi; i += kOrthoThreads) {
-    float u[N];
-    ortho_load<kVec>(s.g, s.g_bf16, base + i * N, u);
-    if (s.momentum) {
-      float m[N];
-      ortho_load<kVec>(s.momentum, 0, base + i * N, m);
-#pragma unroll
-      for (int j = 0; j < N; ++j) m[j] = fmaf(s.mu, m[j], u[j]);
-      ortho_store<kVec>(s.momentum, base + i * N, m);
-      ortho_direction(s, u, m);
-    }
-#pragma unroll
-    for (int j = 0; j < N; ++j) sum += (double)u[j] * (double)u[j];
-  }
+  for (long long i = lo + threadIdx.x; i < hi; i += kOrthoThreads) sum += ortho_square<kVec>(s, base + i * N);
+  // (what is left of a matrix that does not end on a group)
+  if (kVec && blockIdx.x == 0 && threadIdx.x < s.elems - groups * N) sum += ortho_square<false>(s, base + groups * N + threadIdx.x);
   __shared__ double part[kOrthoThreads / 32];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -118,12 +127,12 @@ __device__ __forceinline__ void ortho_scale(const double* sums, int parts, float
   alpha = (float)(1.0 / ldexp(norm, k));
 }
 
-// fp16 planes of u 2^k (rows `ld` apart), and alpha.
+// fp16 planes of u 2^k (rows `ld` apart, padded to whole groups of 8), and alpha.  A thread has 8 columns of a row; where rows do
+// not start on a group (kVec false) it reads them one by one.
 template <bool kVec>
 __global__ void __launch_bounds__(kOrthoThreads)
 ortho_pack_kernel(const __grid_constant__ OrthoSource s, int parts, const double* __restrict__ sums, float eps, int cols, long long ld,
                   __half* __restrict__ x, long long x_batch, long long x_plane /* 0: no low part */, float* __restrict__ alpha) {
-  constexpr int N = OrthoVec<kVec>::N;
   pdl_wait();
   pdl_launch_dependents();
   const int b = blockIdx.y;
@@ -138,33 +147,36 @@ ortho_pack_kernel(const __grid_constant__ OrthoSource s, int parts, const double
   }
   __syncthreads();
   const float scale = scale_s;
-  const long long base = s.use_off ? s.off[b] : b * s.elems, groups = s.elems / N;
-  const int per_row = cols / N;
+  const long long base = s.use_off ? s.off[b] : b * s.elems;
+  const int per_row = (cols + 7) / 8;
+  const long long groups = s.elems / cols * per_row;
   __half* out = x + b * x_batch;
 #pragma unroll 2
   for (long long i = (long long)blockIdx.x * kOrthoThreads + threadIdx.x; i < groups; i += (long long)gridDim.x * kOrthoThreads) {
-    float u[N];
-    ortho_load<kVec>(s.g, s.g_bf16, base + i * N, u);
-    if (s.momentum) {
-      float m[N];
-      ortho_load<kVec>(s.momentum, 0, base + i * N, m);
-      ortho_direction(s, u, m);
-    }
     // (a 64-bit division costs as much as the rest of the loop)
     const long long r = groups >> 32 ? i / per_row : (long long)((uint32_t)i / (uint32_t)per_row);
-    __half* at = out + r * ld + (i - r * per_row) * N;
+    const int c = (int)(i - r * per_row) * 8;
+    const long long from = base + r * cols + c;
+    float u[8], m[8];
     if constexpr (kVec) {
-      uint32_t hi[4], lo[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) tc::split_f16x2(u[2 * j] * scale, u[2 * j + 1] * scale, hi[j], lo[j]);
-      *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      if (x_plane) *reinterpret_cast<uint4*>(at + x_plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      ortho_load<true>(s.g, s.g_bf16, from, u);
+      if (s.momentum) ortho_load<true>(s.momentum, 0, from, m);
     } else {
-      __half hi, lo;
-      tc::split_half(u[0] * scale, hi, lo);
-      *at = hi;
-      if (x_plane) at[x_plane] = lo;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float a[1] = {0.f};
+        if (c + j < cols) ortho_load<false>(s.g, s.g_bf16, from + j, a);
+        u[j] = a[0];
+        m[j] = s.momentum && c + j < cols ? s.momentum[from + j] : 0.f;
+      }
     }
+    if (s.momentum) ortho_direction(s, u, m);
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) tc::split_f16x2(u[2 * j] * scale, u[2 * j + 1] * scale, hi[j], lo[j]);
+    __half* at = out + r * ld + c;
+    *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    if (x_plane) *reinterpret_cast<uint4*>(at + x_plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
 }
 
