@@ -170,13 +170,15 @@ __device__ __forceinline__ void ld_v8(const void* p, uint32_t* v) {
                : "memory");
 }
 
-// One 32-column group of an intermediate, as fp16 planes.  Columns past N are written as far as the buffer's rows are padded
-// (whole groups of 32); what lies there is never read.  `mirror`: the block above the diagonal of a symmetric result goes below
-// it, too.
-__device__ __forceinline__ void epi_h16(const GemmParams& p, int b, int row, int col, bool mirror, float (&v)[32]) {
-  if (row >= p.M) return;
+// One 32-column group of an intermediate, as fp16 planes, by a whole warp; `row` is the lane's, row0 < M the warp's first.  Columns
+// past N are written as far as the buffer's rows are padded (whole groups of 32); what lies there is never read.  `mirror`: the
+// block above the diagonal of a symmetric result goes below it, too, turned over in the warp's scratch: the lanes then hold rows of
+// the mirrored block (stored by twos from where they are, 32 accesses of 64 bytes a group made the tile's end 2 us later).
+__device__ __forceinline__ void epi_h16(const GemmParams& p, int b, int row0, int lane, int col, bool mirror, float (&v)[32], float* scratch) {
+  const int row = row0 + lane;
+  const bool valid = row < p.M;
   const long long at = b * p.h_batch + (long long)row * p.h_ld + col;
-  if (p.aux) {
+  if (p.aux && valid) {
 #pragma unroll
     for (int pl = 0; pl < 2; ++pl) {
       if (pl && !p.h_plane) break;
@@ -198,25 +200,36 @@ __device__ __forceinline__ void epi_h16(const GemmParams& p, int b, int row, int
 #pragma unroll
   for (int pl = 0; pl < 2; ++pl) {
     if (pl && !p.h_plane) break;
-    __half* out = p.h_out + pl * p.h_plane + b * p.h_batch;
+    __half* out = p.h_out + pl * p.h_plane;
     uint32_t h[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       h[i] = pack_f16x2(v[2 * i], v[2 * i + 1]);
       if (p.h_plane) {       // what is left for the low part
-        float a, b2;
-        half2_floats(h[i], a, b2);
-        v[2 * i] -= a;
-        v[2 * i + 1] -= b2;
+        float x, y;
+        half2_floats(h[i], x, y);
+        v[2 * i] -= x;
+        v[2 * i + 1] -= y;
       }
     }
-    st_v8(out + (long long)row * p.h_ld + col, h);
-    st_v8(out + (long long)row * p.h_ld + col + 16, h + 8);
-    if (mirror) {   // the lanes hold consecutive rows: 64 bytes of row `col + j` of the mirrored block
-      __half* m = out + (long long)col * p.h_ld + row;
+    if (valid) {
+      st_v8(out + at, h);
+      st_v8(out + at + 16, h + 8);
+    }
+    if (mirror) {
+      uint32_t* t = reinterpret_cast<uint32_t*>(scratch);
+      __syncwarp();
 #pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (col + j < p.N) m[j * p.h_ld] = __ushort_as_half((unsigned short)(j & 1 ? h[j >> 1] >> 16 : h[j >> 1] & 0xFFFFu));
+      for (int i = 0; i < 16; ++i) t[lane * 17 + i] = h[i];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 16; ++i)   // column `lane` of rows 2 i and 2 i + 1
+        h[i] = __byte_perm(t[2 * i * 17 + (lane >> 1)], t[(2 * i + 1) * 17 + (lane >> 1)], lane & 1 ? 0x7632 : 0x5410);
+      if (col + lane < p.N) {
+        __half* m = out + b * p.h_batch + (long long)(col + lane) * p.h_ld + row0;
+        st_v8(m, h);
+        st_v8(m + 16, h + 8);
+      }
     }
   }
 }
@@ -573,39 +586,45 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
       }
       if constexpr (kKSplit) {
-        // Group g of 32 columns is finished by CTA g % c: the others send it their sums, into its ring (its own products have read
-        // it: the first barrier).  The warps that have the group add them up, in the CTAs' order, and go on with it.
+        // Group g of 32 columns is finished by CTA g % c.  Every CTA leaves the groups of the others in its own shared memory (over
+        // the ring: all its products have read it), 128 rows a column; after the barrier the warps that have the CTA's group
+        // fetch it from each of the others and add up, in the CTAs' order.
         float* ring = reinterpret_cast<float*>(smem);
         const int c = (int)cluster_nctas();
-        cluster_sync_all();
         int mine = -1;
 #pragma unroll 1
         for (int g = 0; g < kGroups; ++g) {
-          const int to = (half * kGroups + g) % c, slot = (half * kGroups + g) / c;
-          if (to == (int)crank) {
+          const int grp = half * kGroups + g;
+          if (grp % c == (int)crank) {
             mine = g;
           } else if (!failed) {
             float v[32];
             tmem_ld32(taddr + g * 32, v);
-            const uint32_t at = mapa_u32(smem_u32(ring + ((slot * c + (int)crank) * 32) * 128 + q * 32 + lane), to);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) st_cluster_f32(at + j * 512, v[j]);
+            for (int j = 0; j < 32; ++j) ring[(grp * 32 + j) * 128 + q * 32 + lane] = v[j];
           }
         }
+        __syncwarp();
         cluster_sync_all();
         if (failed || mine < 0) break;
-        const int slot = (half * kGroups + mine) / c;
         taddr += mine * 32;
+        const uint32_t from = smem_u32(ring + (half * kGroups + mine) * 32 * 128 + q * 32 + lane);
         col0 += mine * 32;
         if (mine) bias[0] = bias[kGroups - 1];
-        float own[32], v[32];
-        tmem_ld32(taddr, own);
+        float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = 0.f;
         for (int r = 0; r < c; ++r) {
-          const float* from = ring + ((slot * c + r) * 32) * 128 + q * 32 + lane;
+          float x[32];
+          if (r == (int)crank) {
+            tmem_ld32(taddr, x);
+          } else {
+            const uint32_t at = mapa_u32(from, r);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] += r == (int)crank ? own[j] : from[j * 128];
+            for (int j = 0; j < 32; ++j) x[j] = ld_cluster_f32(at + j * 512);
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] += x[j];
         }
         tmem_st32(taddr, v);
         groups = 1;
@@ -639,7 +658,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             v[j] = exp2f(fmaf(v[j] - ref, kLog2e, kCeExpBits));
             sum += v[j];
           }
-          if (p.h_out && col < p.N) epi_h16(p, 0, row, col, false, v);
+          if (p.h_out && col < p.N && row0 < p.M) epi_h16(p, 0, row0, lane, col, false, v, scratch);
         }
         if (row < p.M) p.stats[(long long)(col0 / (kKSplit ? 32 : kTileN / 2)) * p.stats_ld + row] = make_float2(ref, sum * 6.103515625e-5f);
       } else {
@@ -650,10 +669,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           float v[32];
           tmem_ld32(taddr + g * 32, v);
           if (g + 1 == groups) release();
-          if (col >= p.N) continue;
+          if (col >= p.N || row0 >= p.M) continue;
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] *= f;
-          if constexpr (kEpi == EPI_H16) epi_h16(p, b, row, col, mirror, v);
+          if constexpr (kEpi == EPI_H16) epi_h16(p, b, row0, lane, col, mirror, v, scratch);
           else if (p.out_vec) epi_out_vec(p, b, row, col, v);
           else epi_out_any(p, b, row0, col, v, scratch, lane);
         }
@@ -664,9 +683,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   }
 
   if constexpr (kKSplit) {
-    if (warp < 2) {   // the two barriers of the exchange are for every thread
+    if (warp < 2) {   // the barrier of the exchange is for every thread
       __syncwarp();
-      cluster_sync_all();
       cluster_sync_all();
     }
   }
@@ -685,7 +703,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
   }
   if (p.wait_late) pdl_wait();
-  if constexpr (kCluster) cluster_sync_all();   // no CTA leaves while another may still signal it or write its ring
+  if constexpr (kCluster) cluster_sync_all();   // no CTA leaves while another may still signal it or read its ring
   if (warp == 2) {
     tc_fence_after();
     if constexpr (kPair) tmem2_dealloc(tmem_base, kTmem);
