@@ -105,12 +105,6 @@ static GemmCut gemm_cut(long long M, long long N, long long K, int batch, bool s
   return best;
 }
 
-// K blocks of 64 that the tensor core adds up before its accumulator is emptied into registers where fp32 results are wanted.
-#ifndef LP_GEMM_ROUND
-#define LP_GEMM_ROUND 1
-#endif
-constexpr int kGemmRound = LP_GEMM_ROUND;
-
 template <int kEpi, int kMode>
 static cudaError_t start_gemm(const tc::GemmParams& p, const CUtensorMap& ma, const CUtensorMap& mb, const GemmCut& cut, cudaStream_t st) {
   using namespace tc;
@@ -136,7 +130,7 @@ static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bo
   p.total_tiles = (int)(per * p.batch);
   p.group_m = std::min(p.tiles_m, pair ? 8 : 16);
   p.kblocks = (int)((K + 63) / 64);
-  p.round_len = kGemmRound;
+  if (!p.round_len) p.round_len = 1;
   p.a_mn = a_mn;
   p.b_mn = b_mn;
   // operand format: bits 7 and 10 (bf16) on top of fp32 accumulation and the shape

@@ -55,13 +55,14 @@ struct GemmParams {
   int group_m;                    // row tiles that are walked together (they share B tiles in L2)
   int kblocks;
   int a_planes, b_planes;         // parts of each operand (1 or 2), `batch` matrices apart
-  int round_len;                  // kRounds: K blocks per accumulation
+  int round_len;                  // kRounds: K blocks per accumulation (0: one)
   int a_mn, b_mn;                 // 1: the operand's row index is the contiguous one
   uint32_t idesc;
   // 1: the kernel before reads and writes nothing of this one's (and has itself waited for what this one reads, before it let
   // this one start): the two run side by side, and this one waits for that one's end before its own
   int wait_late;
   int* err;
+  int* clear;                     // two words (the error word is the first) to clear, or null
   // scale of the accumulator: f * f_dev[b]^f_pow
   float f;
   const float* f_dev;
@@ -418,6 +419,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   if constexpr (kCluster) cluster_sync_all();   // both CTAs' barriers exist before anything signals them from the other side
   tc_fence_after();
   if (!p.wait_late) pdl_wait();
+  if (p.clear && blockIdx.x == 0 && threadIdx.x == 0) p.clear[0] = p.clear[1] = 0;   // (a wait gives up after 0.3 s at the earliest)
   pdl_launch_dependents();
   const uint32_t tmem_base = tail->tmem_base;
   // (its share of K: at least one K block, see gemm_cut)

@@ -22,6 +22,7 @@ constexpr float kCeDlScale = 16384.f;   // fp16 planes of dl (fp32 problems) hol
 // Device-side scalars at the start of the scratch.
 struct CeHeader {
   int err;
+  int done;           // blocks of the last pass over the rows that have finished
   int count;          // rows whose label is a class
   float logit_f;      // scale of x w^T's accumulator
   float dx_f, dw_f;   // scales of the gradients' accumulators
@@ -55,7 +56,7 @@ __device__ __forceinline__ int ce_count_rows(const int32_t* labels, int T, int V
   return n;
 }
 
-// Block 0 counts the rows; for fp32 problems the others take the largest finite magnitudes of x and w (parts of each).
+// fp32 problems: block 0 counts the rows, the others take the largest finite magnitudes of x and w (parts of each).
 __global__ void __launch_bounds__(kCeThreads)
 ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int V, const float* __restrict__ x, long long nx, const float* __restrict__ w,
                   long long nw, float* __restrict__ amax, int parts, CeHeader* __restrict__ hdr) {
@@ -65,7 +66,7 @@ ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int V, const float*
   if (blockIdx.x == 0) {
     const int n = ce_count_rows(labels, T, V);
     if (threadIdx.x == 0) {
-      hdr->err = 0;
+      hdr->err = hdr->done = 0;
       hdr->count = n;
     }
     return;
@@ -125,7 +126,7 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int
     const int counted = is_bf16 ? ce_count_rows(labels, T, V) : hdr->count;
     if (threadIdx.x) return;
     if (is_bf16) {
-      hdr->err = 0;
+      hdr->err = hdr->done = 0;
       hdr->count = counted;
     }
     const float gf = counted > 0 ? g / (float)counted : 0.f;
@@ -197,10 +198,12 @@ __device__ __forceinline__ void ce_join(float& m, float& s, const float2 v) {
   m = top;
 }
 
-// lse and loss of each row from its parts: 8 rows a block (32 bytes of each part), 32 threads a row.
+// lse and loss of each row from its parts: 8 rows a block (64 bytes of each part), 32 threads a row.  On the last piece of the
+// rows (`loss` given) the block that finishes last takes the mean over the counted rows of all T, in the order of the rows.
 __global__ void __launch_bounds__(kCeThreads)
-ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, int rows, int V, const int32_t* __restrict__ labels,
-               const float* __restrict__ target, float* __restrict__ lse, float* __restrict__ row_loss) {
+ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, int r0, int rows, int T, int V,
+               const int32_t* __restrict__ labels, const float* __restrict__ target, float* __restrict__ lse, float* __restrict__ row_loss,
+               CeHeader* __restrict__ hdr, float* __restrict__ loss) {
   pdl_wait();
   pdl_launch_dependents();
   const int r = threadIdx.x & 7, y = threadIdx.x >> 3, row = blockIdx.x * 8 + r;
@@ -213,11 +216,32 @@ ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, 
   ms[y][r] = m;
   ss[y][r] = s;
   __syncthreads();
-  if (y || row >= rows) return;
-  for (int i = 1; i < 32; ++i) ce_join(m, s, make_float2(ms[i][r], ss[i][r]));
-  const float l = m + logf(s);
-  lse[row] = l;
-  row_loss[row] = ce_counts(labels[row], V) ? l - target[row] : 0.f;
+  if (y == 0 && row < rows) {
+    for (int i = 1; i < 32; ++i) ce_join(m, s, make_float2(ms[i][r], ss[i][r]));
+    const float l = m + logf(s);
+    lse[r0 + row] = l;
+    row_loss[r0 + row] = ce_counts(labels[r0 + row], V) ? l - target[r0 + row] : 0.f;
+    __threadfence();
+  }
+  if (!loss) return;
+  __syncthreads();
+  __shared__ int last;
+  if (threadIdx.x == 0) last = atomicAdd(&hdr->done, 1) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  double sum = 0.0;
+  for (int t = threadIdx.x; t < T; t += kCeThreads) sum += (double)__ldcg(row_loss + t);
+  __shared__ double part[kCeThreads / 32];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+  const int n = ce_count_rows(labels, T, V);   // (its barrier is that of `part`, too)
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kCeThreads / 32; ++i) sum += part[i];
+    loss[0] = n > 0 ? (float)(sum / n) : 0.f;
+    loss[1] = (float)n;
+  }
 }
 
 // All of it at once for few rows and parts, in one block: lse and loss of each row, a warp each, the number of counted rows and
@@ -340,26 +364,6 @@ ce_few_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __restr
     float a = -INFINITY, b = 0.f;
     for (int i = 0; i < 8; ++i) ce_join(a, b, parts[i][threadIdx.x]);
     stats[(long long)blockIdx.x * stats_ld + threadIdx.x] = make_float2(a, b);
-  }
-}
-
-// Mean over the counted rows: one block, always in the same order.
-__global__ void __launch_bounds__(kCeThreads)
-ce_loss_kernel(const float* __restrict__ row_loss, int T, const CeHeader* __restrict__ hdr, float* __restrict__ loss) {
-  pdl_wait();
-  pdl_launch_dependents();
-  double s = 0.0;
-  for (int t = threadIdx.x; t < T; t += kCeThreads) s += (double)row_loss[t];
-  __shared__ double part[kCeThreads / 32];
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < kCeThreads / 32; ++i) s += part[i];
-    const int n = hdr->count;
-    loss[0] = n > 0 ? (float)(s / n) : 0.f;
-    loss[1] = (float)n;
   }
 }
 

@@ -248,6 +248,7 @@ static int check_ortho(int dtype, int batch, int rows, int cols, int steps, floa
 // one piece.
 static const size_t kCePieceBytes = (size_t)512 << 20;
 static const int kCeAmaxParts = 592;
+static const int kCeRound = 4;              // K blocks an accumulation (fp32): 2e-7 to 6e-7 of a gradient
 static const int kCeFewBlocks = 592;        // four an SM
 static const size_t kCeFewSmem = 96 * 1024;
 
@@ -412,9 +413,8 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   if (!grads && T <= kCeFewRows && (size_t)(T == 3 ? 4 : T) * D * 4 <= kCeFewSmem)
     return s.f32 ? ce_few_rows(s, T, D, V, (const float*)x, (const float*)w, (const float*)bias, labels, rl, loss_out, st)
                  : ce_few_rows(s, T, D, V, (const bf16*)x, (const bf16*)w, (const bf16*)bias, labels, rl, loss_out, st);
-  const int amax_blocks = s.f32 ? 2 * kCeAmaxParts : 0;
-  if (s.f32 || !s.x)
-    LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + amax_blocks), dim3(kCeThreads), 0, st, labels, T, V, (const float*)x, (long long)T * D,
+  if (s.f32)
+    LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + 2 * kCeAmaxParts), dim3(kCeThreads), 0, st, labels, T, V, (const float*)x, (long long)T * D,
                         (const float*)w, (long long)V * D, s.amax, kCeAmaxParts, s.hdr));
   if (s.x) {
     const int xb = 1 + grid_for((long long)T * D, kCeThreads * 8, Dv.sm_count, 4);
@@ -430,7 +430,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   if ((rc = encode_gemm_map(&m_wk, ow, false)) != LP_OK) return rc;
   if ((rc = encode_gemm_map(&m_wm, ow, true)) != LP_OK) return rc;
   int slab0 = 0;
-  bool finished = false, one_slab = false;
+  bool one_slab = false;
   for (int r0 = 0; r0 < T; r0 += s.rows) {
     const int rows = std::min(s.rows, T - r0);
     const GemmOperand ox{(const uint16_t*)xm + (long long)r0 * ldx, D, rows, ldx, x_plane, planes, !s.f32};
@@ -447,15 +447,17 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     p.bias = bias; p.bias_bf16 = is_bf16; p.labels = labels + r0;
     p.stats = s.stats; p.stats_ld = s.rows; p.target = s.target + r0;
     p.h_out = s.p; p.h_ld = s.ld_v; p.h_plane = s.f32 ? p_plane : 0;
+    p.round_len = kCeRound;
+    if (!s.x && r0 == 0) p.clear = &s.hdr->err;   // (no kernel before that could have)
     if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, cut, st)) != LP_OK) return rc;
     // few rows and parts: one block does the rest of the loss
-    finished = rows == T && rows <= 64 && parts <= 128;
+    const bool finished = rows == T && rows <= 64 && parts <= 128;
     if (finished)
       LP_CUDA_OK(launch_pdl(ce_finish_kernel, dim3(1), dim3(1024), 0, st, (const float2*)s.stats, (long long)s.rows, parts, rows, V, labels,
                             (const float*)s.target, s.lse, rl, loss_out));
     else
       LP_CUDA_OK(launch_pdl(ce_rows_kernel, dim3((rows + 7) / 8), dim3(kCeThreads), 0, st, (const float2*)s.stats, (long long)s.rows, parts,
-                            rows, V, labels + r0, (const float*)(s.target + r0), s.lse + r0, rl + r0));
+                            r0, rows, T, V, labels, (const float*)s.target, s.lse, rl, s.hdr, r0 + rows == T ? loss_out : nullptr));
     if (!grads) continue;
     const int slabs = (rows + kCeSlab - 1) / kCeSlab;
     one_slab = slabs == 1 && rows == T;
@@ -471,7 +473,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       memset(&p, 0, sizeof(p));
       p.M = rows; p.N = D; p.batch = 1; p.err = &s.hdr->err;
       p.a_planes = p.b_planes = planes;
-      p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1;
+      p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1; p.round_len = kCeRound;
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
       const GemmCut kd = gemm_cut(rows, D, V, 1, false, planes, planes);
       if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, kd, st)) != LP_OK) return rc;
@@ -483,7 +485,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       memset(&p, 0, sizeof(p));
       p.M = V; p.N = D; p.batch = 1; p.err = &s.hdr->err;
       p.a_planes = p.b_planes = planes;
-      p.f = 1.f; p.f_dev = &s.hdr->dw_f; p.f_pow = 1;
+      p.f = 1.f; p.f_dev = &s.hdr->dw_f; p.f_pow = 1; p.round_len = kCeRound;
       p.out = dw; p.out_bf16 = is_bf16; p.out_ld = D;
       // (beside dx's product where that leaves SMs idle: 64 rows x 512 x 1000 30 us and 33 one after the other, fp32 43 and 48;
       // where it has all of them the two share L2 badly, 4096 x 2048 x 32000 1.32 ms and 1.31)
@@ -500,8 +502,6 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   if (dbias && !one_slab)
     LP_CUDA_OK(launch_pdl(ce_dbias_kernel, dim3((V + kCeThreads - 1) / kCeThreads), dim3(kCeThreads), 0, st, (const float*)s.sums, slab0, V,
                           (const CeHeader*)s.hdr, dbias, is_bf16));
-  if (!finished)
-    LP_CUDA_OK(launch_pdl(ce_loss_kernel, dim3(1), dim3(kCeThreads), 0, st, (const float*)rl, T, (const CeHeader*)s.hdr, loss_out));
   return LP_OK;
 }
 
