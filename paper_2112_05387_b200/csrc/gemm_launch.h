@@ -38,6 +38,22 @@ static int gemm_set_attributes() {
   LP_CUDA_OK(cudaFuncSetAttribute(gemm_tc_kernel<kEpi, GEMM_KSPLIT, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmSmem));
   return LP_OK;
 }
+// Clusters of `ctas` CTAs of a kernel that the device holds at once (0: none, or it cannot say).
+template <typename... KArgs>
+static int max_clusters(int ctas, void (*kernel)(KArgs...), int threads, size_t smem, int sms) {
+  cudaLaunchConfig_t q = {};
+  q.gridDim = dim3(ctas * sms);
+  q.blockDim = dim3(threads);
+  q.dynamicSmemBytes = smem;
+  cudaLaunchAttribute qa[1];
+  qa[0].id = cudaLaunchAttributeClusterDimension;
+  qa[0].val.clusterDim.x = ctas; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
+  q.attrs = qa;
+  q.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
+  return n;
+}
 // Kernel attributes, and how many CTA pairs the device holds at once (the grid is persistent: never more than that).
 static int gemm_init_dev() {
   int rc = init_cur_dev();
@@ -51,22 +67,9 @@ static int gemm_init_dev() {
       (rc = gemm_set_attributes<EPI_OUT, GEMM_LOW>()) != LP_OK || (rc = gemm_set_attributes<EPI_OUT, GEMM_SPLIT>()) != LP_OK ||
       (rc = gemm_set_attributes<EPI_CE, GEMM_ONE>()) != LP_OK || (rc = gemm_set_attributes<EPI_CE, GEMM_SPLIT>()) != LP_OK)
     return rc;
-  auto clusters = [&](int ctas, auto kernel) {
-    cudaLaunchConfig_t q = {};
-    q.gridDim = dim3(ctas * D.sm_count);
-    q.blockDim = dim3(kGemmThreads);
-    q.dynamicSmemBytes = kGemmSmem;
-    cudaLaunchAttribute qa[1];
-    qa[0].id = cudaLaunchAttributeClusterDimension;
-    qa[0].val.clusterDim.x = ctas; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
-    q.attrs = qa;
-    q.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
-    return n;
-  };
-  D.gemm_pairs = clusters(2, gemm_tc_kernel<EPI_OUT, GEMM_PAIR, GEMM_ONE>);
-  for (int c = 2; c <= 4; ++c) D.gemm_clusters[c] = clusters(c, gemm_tc_kernel<EPI_OUT, GEMM_KSPLIT, GEMM_ONE>);
+  D.gemm_pairs = max_clusters(2, gemm_tc_kernel<EPI_OUT, GEMM_PAIR, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
+  for (int c = 2; c <= 4; ++c) 
+    D.gemm_clusters[c] = max_clusters(c, gemm_tc_kernel<EPI_OUT, GEMM_KSPLIT, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
   D.gemm_attr = true;
   return LP_OK;
 }

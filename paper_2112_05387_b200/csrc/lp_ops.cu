@@ -66,16 +66,20 @@ size_t ortho_scratch_bytes(int batch, int rows, int cols, bool split) {
 }
 
 // One launch for matrices whose X stays in the shared memory of a cluster (ortho_small.cuh): the smaller side is at most 128 and
-// the larger fits in 8 slices.  As many CTAs as the SMs hold at once, but slices of 32 columns at least.
+// the larger fits in 8 slices.  As many CTAs a matrix as keep all clusters resident at once, but slices of 32 columns at least (18
+// matrices of 64 x 576: 55 us on clusters of four, 68 on eight, of which 16 fit).
 static const size_t kSmallMaxSmem = 224 * 1024;
 struct SmallShape { int S, ctas, slice; };
-static bool ortho_small_shape(int batch, int rows, int cols, bool split, int sms, SmallShape* out) {
+static bool ortho_small_shape(int batch, int rows, int cols, bool split, SmallShape* out) {
   const int s = std::min(rows, cols), l = std::max(rows, cols);
   if (s > 128 || l > (1 << 20)) return false;
   const int S = s <= 16 ? 16 : s <= 32 ? 32 : s <= 64 ? 64 : 128;
   auto slice = [&](int c) { return ((l + c - 1) / c + 15) / 16 * 16; };
+  const Device& D = cur_dev();
   int c = 1;
-  while (c < 8 && (small_smem(S, slice(c), split) > kSmallMaxSmem || ((long long)batch * 2 * c <= sms && slice(2 * c) >= 32))) c *= 2;
+  while (c < 8 && D.small_clusters[2 * c] > 0 &&
+         (small_smem(S, slice(c), split) > kSmallMaxSmem || (batch <= D.small_clusters[2 * c] && slice(2 * c) >= 32)))
+    c *= 2;
   if (small_smem(S, slice(c), split) > kSmallMaxSmem) return false;
   *out = SmallShape{S, c, slice(c)};
   return true;
@@ -101,6 +105,7 @@ static int ortho_init_dev() {
   if ((rc = small_set_attributes<16>()) != LP_OK || (rc = small_set_attributes<32>()) != LP_OK ||
       (rc = small_set_attributes<64>()) != LP_OK || (rc = small_set_attributes<128>()) != LP_OK)
     return rc;
+  for (int c = 1; c <= 8; c *= 2) D.small_clusters[c] = max_clusters(c, ortho_small_kernel<true, 128>, kSmallThreads, kSmallMaxSmem, D.sm_count);
   D.ortho_attr = true;
   return LP_OK;
 }
@@ -147,7 +152,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     for (int b = 0; b < B; ++b) src.off[b] = q.off[b];
   }
   SmallShape small_shape;
-  if (ortho_small_shape(B, q.rows, q.cols, q.split, D.sm_count, &small_shape)) {
+  if (ortho_small_shape(B, q.rows, q.cols, q.split, &small_shape)) {
     if (launches) *launches += 1;
     return ortho_run_small(q, src, small_shape, clear_err, st);
   }

@@ -34,9 +34,9 @@ __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], const __half* p) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(tc::smem_u32(p)) : "memory");
 }
-__device__ __forceinline__ void ldsm2_trans(uint32_t (&r)[2], const __half* p) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];"
-               : "=r"(r[0]), "=r"(r[1]) : "r"(tc::smem_u32(p)) : "memory");
+__device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], const __half* p) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(tc::smem_u32(p)) : "memory");
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -57,53 +57,64 @@ __device__ __forceinline__ void st_cluster_b32x2(uint32_t addr, uint32_t a, uint
 }
 
 // Shared memory: planes of X [2][S][slice + 8], of A [P][S][S + 8], then the partial sums [G][S][S] fp32 and, in the same place
-// later, the planes of B [P][S][S + 8].  P: 2 for fp32 results, else 1 (A and B are fp16).  G: K groups of the warps.
-__host__ __device__ constexpr int small_groups(int S) { return S == 16 ? 8 : (S == 32 ? 2 : 1); }
+// later, the planes of B [P][S][S + 8].  P: 2 for fp32 results, else 1 (A and B are fp16).  The warps share X X^T as tiles of 16
+// rows and small_cols() columns, G groups of them K where there are fewer tiles than warps.
+__host__ __device__ constexpr int small_cols(int S) { return S == 16 ? 16 : (S == 128 ? 64 : 32); }
+__host__ __device__ constexpr int small_groups(int S) { return S == 16 ? 8 : (S == 32 ? 4 : 1); }
 __host__ __device__ inline size_t small_smem(int S, int slice, bool split) {
   const size_t mat = (size_t)(split ? 2 : 1) * S * (S + 8) * 2, part = (size_t)small_groups(S) * S * S * 4;
   return (size_t)2 * S * (slice + 8) * 2 + mat + (mat > part ? mat : part);
 }
 
-// Products of the 16 x 16 block (m0, n0) of P Q^T over K columns [k0, k1): planes of P and Q `pl` elements apart, rows `ld`.
+// Products of the 16 x 16 NB tile (m0, n0) of P Q^T over K columns [k0, k1): planes of P and Q `pl` elements apart, rows `ld`.
 // kSplit: all parts but lo * lo.
-template <bool kSplit>
-__device__ __forceinline__ void small_block(float (&sum)[2][4], const __half* P, const __half* Q, int pl, int ld, int m0, int n0, int k0,
-                                            int k1, int lane) {
+template <bool kSplit, int NB>
+__device__ __forceinline__ void small_tile(float (&sum)[NB][2][4], const __half* P, const __half* Q, int pl, int ld, int m0, int n0, int k0,
+                                           int k1, int lane) {
   const __half* pa = P + (m0 + (lane & 15)) * ld + (lane >> 4) * 8;
   // two 8-row tiles of Q: lanes 0-7 rows n0.., 8-15 the same 8 columns on, 16-31 rows n0 + 8..
   const __half* qb = Q + (n0 + (lane & 7) + ((lane >> 4) << 3)) * ld + ((lane >> 3) & 1) * 8;
 #pragma unroll 1
   for (int k = k0; k < k1; k += 32) {
-    float acc[2][4] = {};
+    float acc[NB][2][4] = {};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int kk = k + 16 * h;
       if (kk >= k1) break;
-      uint32_t ah[4], bh[4];
+      uint32_t ah[4], al[4], bh[NB][4], bl[NB][4];
       ldsm4(ah, pa + kk);
-      ldsm4(bh, qb + kk);
-      if constexpr (kSplit) {
-        uint32_t al[4], bl[4];
-        ldsm4(al, pa + pl + kk);
-        ldsm4(bl, qb + pl + kk);
+      if constexpr (kSplit) ldsm4(al, pa + pl + kk);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          mma_f16(acc[t], ah, bl[2 * t], bl[2 * t + 1]);
-          mma_f16(acc[t], al, bh[2 * t], bh[2 * t + 1]);
-        }
+      for (int n = 0; n < NB; ++n) {
+        ldsm4(bh[n], qb + 16 * n * ld + kk);
+        if constexpr (kSplit) ldsm4(bl[n], qb + pl + 16 * n * ld + kk);
+      }
+      if constexpr (kSplit) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) mma_f16(acc[n][t], ah, bl[n][2 * t], bl[n][2 * t + 1]);
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) mma_f16(acc[n][t], al, bh[n][2 * t], bh[n][2 * t + 1]);
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) mma_f16(acc[t], ah, bh[2 * t], bh[2 * t + 1]);
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) mma_f16(acc[n][t], ah, bh[n][2 * t], bh[n][2 * t + 1]);
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[t][i] += acc[t][i];
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[n][t][i] += acc[n][t][i];
   }
 }
 
 template <bool kSplit, int S>
-__global__ void __launch_bounds__(kSmallThreads, 1)
+__global__ void __launch_bounds__(kSmallThreads, S <= 64 ? 2 : 1)
 ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
   extern __shared__ __align__(16) uint8_t small_smem_raw[];
   constexpr int P = kSplit ? 2 : 1, G = small_groups(S), LD = S + 8;
@@ -182,21 +193,26 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
   __syncthreads();
 
   const int g = lane >> 2, t2 = 2 * (lane & 3);   // accumulator fragment: rows g, g + 8, columns t2, t2 + 1
-  constexpr int kBlocks = (S / 16) * (S / 16);
+  constexpr int kCols = small_cols(S), NB = kCols / 16, kAcross = S / kCols, kTiles = S / 16 * kAcross;
+  constexpr int kMine = (kTiles + kSmallWarps - 1) / kSmallWarps;     // of a warp, where no group shares K
+  static_assert(kTiles * G % kSmallWarps == 0 || kTiles * G < kSmallWarps, "tiles over the warps");
   for (int step = 0; step < q.steps; ++step) {
     const bool last = step + 1 == q.steps;
-    // partial sums of X X^T: 16 x 16 blocks over the warps, K in G groups where there are fewer blocks than warps
-    for (int w = warp; w < kBlocks * G; w += kSmallWarps) {
-      const int blk = w % kBlocks, grp = w / kBlocks;
-      const int m0 = blk / (S / 16) * 16, n0 = blk % (S / 16) * 16, ks = q.slice / 16;
-      float acc[2][4] = {};
-      small_block<kSplit>(acc, X, X, xpl, ldx, m0, n0, ks * grp / G * 16, ks * (grp + 1) / G * 16, lane);
+    // partial sums of X X^T
+#pragma unroll 1
+    for (int w = warp; w < kTiles * G; w += kSmallWarps) {
+      const int tile = w % kTiles, grp = w / kTiles;
+      const int m0 = tile / kAcross * 16, n0 = tile % kAcross * kCols, ks = q.slice / 16;
+      float acc[NB][2][4] = {};
+      small_tile<kSplit, NB>(acc, X, X, xpl, ldx, m0, n0, ks * grp / G * 16, ks * (grp + 1) / G * 16, lane);
       float* o = part + grp * S * S + (m0 + g) * S + n0 + t2;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        *reinterpret_cast<float2*>(o + 8 * t) = make_float2(acc[t][0], acc[t][1]);
-        *reinterpret_cast<float2*>(o + 8 * S + 8 * t) = make_float2(acc[t][2], acc[t][3]);
-      }
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          *reinterpret_cast<float2*>(o + 16 * n + 8 * t) = make_float2(acc[n][t][0], acc[n][t][1]);
+          *reinterpret_cast<float2*>(o + 8 * S + 16 * n + 8 * t) = make_float2(acc[n][t][2], acc[n][t][3]);
+        }
     }
     __syncwarp();
     tc::cluster_sync_all();
@@ -229,69 +245,77 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
     }
     __syncwarp();
     tc::cluster_sync_all();   // A is complete everywhere, and the partial sums have been read: B may take their place
-    constexpr int kMine = (kBlocks + kSmallWarps - 1) / kSmallWarps;
-    float bv[kMine][2][4] = {};
 #pragma unroll
     for (int u = 0; u < kMine; ++u) {
-      const int blk = warp + u * kSmallWarps;
-      if (blk >= kBlocks) break;
-      small_block<kSplit>(bv[u], A, A, S * LD, LD, blk / (S / 16) * 16, blk % (S / 16) * 16, 0, S, lane);
+      const int tile = warp + u * kSmallWarps;
+      if (tile >= kTiles) break;
+      const int m0 = tile / kAcross * 16, n0 = tile % kAcross * kCols;
+      float bv[NB][2][4] = {};
+      small_tile<kSplit, NB>(bv, A, A, S * LD, LD, m0, n0, 0, S, lane);
+      const float fa = q.b * (kB / kA), fc = q.c * (kB / (kA * kA));
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = m0 + g + 8 * h, c = n0 + 16 * n + 8 * t + t2, at = r * LD + c;
+            float a0, a1;
+            tc::half2_floats(*reinterpret_cast<const uint32_t*>(A + at), a0, a1);
+            if constexpr (kSplit) {
+              float l0, l1;
+              tc::half2_floats(*reinterpret_cast<const uint32_t*>(A + S * LD + at), l0, l1);
+              a0 += l0;
+              a1 += l1;
+            }
+            uint32_t hi, lo;
+            tc::split_f16x2(fmaf(fc, bv[n][t][2 * h], fa * a0) + (r == c ? q.a * kB : 0.f),
+                            fmaf(fc, bv[n][t][2 * h + 1], fa * a1) + (r == c + 1 ? q.a * kB : 0.f), hi, lo);
+            *reinterpret_cast<uint32_t*>(B + at) = hi;
+            if constexpr (kSplit) *reinterpret_cast<uint32_t*>(B + S * LD + at) = lo;
+          }
     }
+    __syncthreads();
+    // X <- B X in place: a warp has 16 rows (their part of B stays in its registers) of a strip of 16 columns, the warps together
+    // all rows of 8 / (S / 16) strips a pass.  Everything of a strip is in registers before any of it is written.
+    constexpr int kK = S / 16, kStrips = kSmallWarps / kK;
+    const int m0 = warp % kK * 16;
+    uint32_t bh[kK][4], bl[kSplit ? kK : 1][4];
 #pragma unroll
-    for (int u = 0; u < kMine; ++u) {
-      const int blk = warp + u * kSmallWarps;
-      if (blk >= kBlocks) break;
+    for (int k = 0; k < kK; ++k) {
+      const __half* from = B + (m0 + (lane & 15)) * LD + 16 * k + (lane >> 4) * 8;
+      ldsm4(bh[k], from);
+      if constexpr (kSplit) ldsm4(bl[k], from + S * LD);
+    }
+#pragma unroll 1
+    for (int s0 = 0; s0 < q.slice / 16; s0 += kStrips) {
+      const int n0 = (s0 + warp / kK) * 16;
+      const bool mine = n0 < q.slice;
+      float lo_acc[2][4] = {}, hi_acc[2][4] = {};
+      if (mine) {
+        // lanes 0-7 rows k.. of 8 columns, 8-15 the next 8 rows, 16-31 the same of the next 8 columns
+        const __half* from = X + (lane & 15) * ldx + n0 + (lane >> 4) * 8;
+#pragma unroll
+        for (int k = 0; k < kK; ++k) {
+          uint32_t xh[4], xl[4];
+          ldsm4_trans(xh, from + 16 * k * ldx);
+          ldsm4_trans(xl, from + xpl + 16 * k * ldx);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            mma_f16(lo_acc[t], bh[k], xl[2 * t], xl[2 * t + 1]);
+            if constexpr (kSplit) mma_f16(lo_acc[t], bl[k], xh[2 * t], xh[2 * t + 1]);
+            mma_f16(hi_acc[t], bh[k], xh[2 * t], xh[2 * t + 1]);
+          }
+        }
+      }
+      __syncthreads();
+      if (!mine) continue;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int r = blk / (S / 16) * 16 + g + 8 * h, c = blk % (S / 16) * 16 + 8 * t + t2, at = r * LD + c;
-          float a0, a1;
-          tc::half2_floats(*reinterpret_cast<const uint32_t*>(A + at), a0, a1);
-          if constexpr (kSplit) {
-            float l0, l1;
-            tc::half2_floats(*reinterpret_cast<const uint32_t*>(A + S * LD + at), l0, l1);
-            a0 += l0;
-            a1 += l1;
-          }
-          const float fa = q.b * (kB / kA), fc = q.c * (kB / (kA * kA));
-          uint32_t hi, lo;
-          tc::split_f16x2(fmaf(fc, bv[u][t][2 * h], fa * a0) + (r == c ? q.a * kB : 0.f),
-                          fmaf(fc, bv[u][t][2 * h + 1], fa * a1) + (r == c + 1 ? q.a * kB : 0.f), hi, lo);
-          *reinterpret_cast<uint32_t*>(B + at) = hi;
-          if constexpr (kSplit) *reinterpret_cast<uint32_t*>(B + S * LD + at) = lo;
-        }
-    }
-    __syncthreads();
-    // X <- B X, 8 columns a warp: they are read into registers before any of them is written
-    for (int n0 = warp * 8; n0 < q.slice; n0 += kSmallWarps * 8) {
-      uint32_t xh[S / 16][2], xl[S / 16][2];
-#pragma unroll
-      for (int k = 0; k < S / 16; ++k) {
-        const __half* from = X + (16 * k + (lane & 15)) * ldx + n0;
-        ldsm2_trans(xh[k], from);
-        ldsm2_trans(xl[k], from + xpl);
-      }
-#pragma unroll 1
-      for (int m0 = 0; m0 < S; m0 += 16) {
-        float lo_acc[4] = {}, hi_acc[4] = {};
-#pragma unroll
-        for (int k = 0; k < S / 16; ++k) {
-          uint32_t bh[4];
-          const __half* from = B + (m0 + (lane & 15)) * LD + 16 * k + (lane >> 4) * 8;
-          ldsm4(bh, from);
-          mma_f16(lo_acc, bh, xl[k][0], xl[k][1]);
-          if constexpr (kSplit) {
-            uint32_t bl[4];
-            ldsm4(bl, from + S * LD);
-            mma_f16(lo_acc, bl, xh[k][0], xh[k][1]);
-          }
-          mma_f16(hi_acc, bh, xh[k][0], xh[k][1]);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int i = m0 + g + 8 * h, j = n0 + t2;
-          const float v[2] = {(hi_acc[2 * h] + lo_acc[2 * h]) * (1.f / kB), (hi_acc[2 * h + 1] + lo_acc[2 * h + 1]) * (1.f / kB)};
+          const int i = m0 + g + 8 * h, j = n0 + 8 * t + t2;
+          const float v[2] = {(hi_acc[t][2 * h] + lo_acc[t][2 * h]) * (1.f / kB), (hi_acc[t][2 * h + 1] + lo_acc[t][2 * h + 1]) * (1.f / kB)};
           if (!last) {
             uint32_t hi, lo;
             tc::split_f16x2(v[0], v[1], hi, lo);
@@ -315,7 +339,6 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
             }
           }
         }
-      }
     }
     __syncthreads();
   }
