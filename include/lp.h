@@ -389,7 +389,7 @@ int lp_conv2d_fwd_noalloc(int N, int H, int W, int Cin, int Cout, int R, int str
  *   l = x w^T + bias;  row_loss[t] = log sum_v exp l[t][v] - l[t][labels[t]];  loss = mean of row_loss over the counted rows
  * A row counts if its label is a class, 0 <= labels[t] < V; any other label leaves the row out: its row_loss and its row of dx
  * are 0 and nothing of x[t] (which may hold anything, NaN included) reaches dw or dbias.
- *   T, V up to 2^28, D up to 2^20; x [T][D], w [V][D], bias [V] or NULL (entries may be -inf: that class then has probability 0), labels int32 [T]
+ *   T up to 2^28, V up to 2^24, D up to 2^20; x [T][D], w [V][D], bias [V] or NULL (entries may be -inf: that class then has probability 0), labels int32 [T]
  *   loss_out: float[2] = { loss (0 if no row counts), number of counted rows }; row_loss: float[T] or NULL
  *   dx [T][D], dw [V][D], dbias [V]: grad_scale times the gradient of loss, any of them NULL; overwritten.  All NULL: the loss
  *     alone.
@@ -404,7 +404,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
 /* Orthogonalisation by Newton-Schulz products, of `batch` matrices G [rows][cols] one after another in memory:
  *   X = G / max(|G|_F, eps);  `steps` times  X <- a X + b (X X^T) X + c (X X^T)^2 X;  out = X
  * coeffs: host float[3] = { a, b, c }, or NULL for { 3.4445, -4.7750, 2.0315 }, which take the singular values near 1 in five
- * steps.  out may be g.  1 <= steps <= 32, eps >= 1e-30; coefficients under which a singular value of X passes 15, or one of
+ * steps.  out may be g.  batch <= 65535, sides up to 2^24, the smaller one up to 2^17; 1 <= steps <= 32, 1e-30 <= eps <= 1e30; coefficients under which a singular value of X passes 15, or one of
  * b X X^T + c (X X^T)^2 passes 60, overflow.  A matrix that holds NaN or an infinity becomes NaN, no other matrix does.
  * LP_BF16: iterates are kept in fp16 (11 significant bits, the first ones in two parts), the result is off by about half of
  * bf16's own step.  LP_F32: every operand is kept in two parts. */

@@ -2978,13 +2978,17 @@ static size_t muon_module_scratch(const Plan& P, bool split) {
 
 size_t lp_step_muon_scratch_bytes(lp_handle* h) {
   if (!h) return 0;
-  size_t total = 0;
-  for (const Plan& P : h->modules) total += muon_module_scratch(P, h->dtype == LP_F32);
-  return total;
+  try {
+    size_t total = 0;
+    for (const Plan& P : h->modules) total += muon_module_scratch(P, h->dtype == LP_F32);
+    return total;
+  } catch (...) {   // (host memory)
+    return 0;
+  }
 }
 
 static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momentum, bool nesterov, float weight_decay, float kappa_step,
-                       void* lambda_inout, void* scratch, cudaStream_t st) {
+                       void* lambda_inout, void* scratch, cudaStream_t st) try {
   Plan& P = h->modules[k];
   const bool kappa = lambda_inout && k + 1 < h->net.K;
   TimelineScope ts(h, st, k, LP_OP_UPDATE, LP_PHASE_UPDATE, (momentum != 0.f ? 20.0 : 12.0) * (double)P.ps.n +
@@ -3022,6 +3026,8 @@ static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momen
   if (rc != LP_OK) return rc;
   P.ps.grads_fresh = false;
   return kappa ? update_kappa(h, k, kappa_step, lambda_inout, st) : LP_OK;
+} catch (...) {   // (host memory)
+  return LP_ERR_CUDA;
 }
 
 int lp_step_muon(lp_handle* h, float lr_conv, float lr, float momentum, int nesterov, float weight_decay, float kappa_step,
@@ -3031,7 +3037,14 @@ int lp_step_muon(lp_handle* h, float lr_conv, float lr, float momentum, int nest
   for (auto& P : h->modules) any = any || P.ps.grads_fresh;
   if (!any) return LP_ERR_ORDER;
   if (reinterpret_cast<uintptr_t>(scratch) & 255) return LP_ERR_ALIGN;
-  if (scratch_bytes < lp_step_muon_scratch_bytes(h)) return LP_ERR_WORKSPACE;
+  const size_t need = lp_step_muon_scratch_bytes(h);
+  if (!need || scratch_bytes < need) return LP_ERR_WORKSPACE;
+  size_t sizes[LP_MAX_MODULES];
+  try {
+    for (size_t k = 0; k < h->modules.size(); ++k) sizes[k] = muon_module_scratch(h->modules[k], h->dtype == LP_F32);
+  } catch (...) {
+    return LP_ERR_WORKSPACE;
+  }
   const int K = h->net.K;
   if (lambdas_inout)
     for (int k = 0; k + 1 < K; ++k)
@@ -3055,7 +3068,7 @@ int lp_step_muon(lp_handle* h, float lr_conv, float lr, float momentum, int nest
     if (h->modules[k].ps.grads_fresh)
       first_err = muon_module(h, k, lr_conv, lr, momentum, nesterov != 0, weight_decay, kappa_step,
                               (lambdas_inout && k + 1 < K) ? lambdas_inout[k] : nullptr, at, apart ? h->streams[k] : st);
-    at += muon_module_scratch(h->modules[k], h->dtype == LP_F32);
+    at += sizes[k];
   }
   for (int k = 0; k < forked; ++k)
     if (cudaEventRecord(h->done[k], h->streams[k]) != cudaSuccess || cudaStreamWaitEvent(st, h->done[k], 0) != cudaSuccess)

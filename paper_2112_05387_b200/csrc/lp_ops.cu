@@ -81,6 +81,10 @@ static bool ortho_small_shape(int batch, int rows, int cols, bool split, SmallSh
          (small_smem(S, slice(c), split) > kSmallMaxSmem || (batch <= D.small_clusters[2 * c] && slice(2 * c) >= 32)))
     c *= 2;
   if (small_smem(S, slice(c), split) > kSmallMaxSmem) return false;
+  // (128 rows and more than 64 columns a CTA: 128 x 1152 in fp32 130 us, 122 as products of gemm_tc.cuh; 128 x 512 91 and 112;
+  // 40 of 128 x 1152, more than fit at once, 402 and 178; 128 of 64 x 1152, 255 and 216)
+  const bool waits = batch > D.small_clusters[c];
+  if (S == 128 ? slice(c) > 64 || waits : S == 64 && slice(c) > 288 && waits) return false;
   *out = SmallShape{S, c, slice(c)};
   return true;
 }
@@ -241,7 +245,8 @@ const float kOrthoCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
 static int check_ortho(int dtype, int batch, int rows, int cols, int steps, float eps) {
   if (dtype != LP_F32 && dtype != LP_BF16) return LP_ERR_UNSUPPORTED;
   if (batch < 1 || rows < 1 || cols < 1 || batch > 65535 || steps < 1 || steps > 32) return LP_ERR_SIZE;
-  if ((long long)rows * cols > (1LL << 36) || std::min(rows, cols) > (1 << 17)) return LP_ERR_SIZE;
+  // (sides of 2^24: a product's longest accumulation, 2^18 K blocks, is less than half of what a bounded wait waits)
+  if (rows > (1 << 24) || cols > (1 << 24) || std::min(rows, cols) > (1 << 17)) return LP_ERR_SIZE;
   if (!(eps >= 1e-30f) || !(eps <= 1e30f)) return LP_ERR_SIZE;
   return LP_OK;
 }
@@ -384,7 +389,7 @@ int lp_muon_update(int dtype, int batch, int rows, int cols, void* w, const void
 }
 
 static bool ce_size_ok(int T, int D, int V) {
-  return T >= 1 && D >= 1 && V >= 1 && T <= (1 << 28) && V <= (1 << 28) && D <= (1 << 20);
+  return T >= 1 && D >= 1 && V >= 1 && T <= (1 << 28) && V <= (1 << 24) && D <= (1 << 20);   // (V: see check_ortho)
 }
 
 size_t lp_linear_cross_entropy_scratch_bytes(int dtype, int T, int D, int V, int grads) {

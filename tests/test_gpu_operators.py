@@ -632,6 +632,73 @@ def test_nothing_is_written_outside_the_results():
             assert bool((whole[:64] == 3).all()) and bool((whole[-64:] == 3).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tensors_on_16_byte_boundaries(dtype):
+    """Every tensor 16 bytes past a 256-byte boundary (whole sectors are 32): the same bits as on the boundary."""
+    import torch
+    off = 4 if dtype == "f32" else 8
+
+    def moved(t, n):
+        whole = torch.zeros(t.numel() + 64, dtype=t.dtype, device="cuda")
+        part = whole[n:n + t.numel()].view(t.shape)
+        part.copy_(t)
+        return part
+    x, w, b, labels = ce_inputs(200, 96, 1504, dtype, ignored=0.1)
+    want = ce_run(x, w, b, labels)
+    import paper_2112_05387_b200 as lp
+    code = lp.LP_F32 if dtype == "f32" else lp.LP_BF16
+    buf, at, n = scratch_of(lp.lp_linear_cross_entropy_scratch_bytes(code, 200, 96, 1504, True))
+    got = {k: moved(torch.zeros_like(v), 4 if v.dtype == torch.float32 else 8) for k, v in want.items()}
+    lp.lp_linear_cross_entropy(code, 200, 96, 1504, moved(x, off), moved(w, off), moved(b, off), moved(labels, 4), 1.0, got["loss"], got["row_loss"],
+                               got["dx"], got["dw"], got["dbias"], at, n)
+    assert lp.lp_scratch_status(at) == lp.LP_OK
+    assert all(torch.equal(got[k], want[k]) for k in want)
+    for size in ((2, 40, 96), (2, 160, 288), (1, 288, 160)):
+        g = torch.randn(*size, device="cuda").to(x.dtype)
+        assert torch.equal(ortho_run(moved(g, off), out=moved(torch.zeros_like(g), off)), ortho_run(g)), size
+    del buf
+
+
+def test_the_step_recorded_and_replayed_equals_the_calls():
+    """Passes and lp_step_muon in a recording of the handle, launched twice, against a handle that makes the calls."""
+    import torch
+    import paper_2112_05387_b200 as lp
+    from conftest import small_cfg
+    from harness import GpuRun
+    cfg = small_cfg("postbn", dtype="f32", stage_channels=(16, 32))
+    runs = [GpuRun(cfg) for _ in range(2)]
+    gen = torch.Generator("cuda").manual_seed(9)
+    K = runs[0].net.K
+    x = [torch.randn(*runs[0].net.boundary[k], generator=gen, device="cuda") for k in range(K)]
+    labels = torch.randint(0, cfg["num_classes"], (cfg["N"],), generator=gen, device="cuda", dtype=torch.int32)
+    st = torch.cuda.Stream()
+    s = st.cuda_stream
+    state = []
+    for r, run in enumerate(runs):
+        buf, at, nb = scratch_of(lp.lp_step_muon_scratch_bytes(run.h))
+        loss = torch.zeros(K, 2, device="cuda")
+        torch.cuda.synchronize()
+
+        def step():
+            lp.lp_modules_fwd_bwd_all(run.h, x, labels, None, 0.7, loss, None, s)
+            lp.lp_step_muon(run.h, 0.02, 0.01, 0.9, True, 1e-3, 0.0, None, at, nb, s)
+        step()
+        if r == 0:
+            lp.lp_graph_begin(run.h, s)
+            step()
+            gid = lp.lp_graph_end(run.h, s)
+            for _ in range(2):
+                lp.lp_graph_launch(run.h, gid, s)
+        else:
+            for _ in range(2):
+                step()
+        assert lp.lp_last_device_status(run.h, s) == 0
+        state.append([lp.lp_get_params(run.h, k) for k in range(K)])
+        del buf
+    for a, b in zip(*state):
+        assert np.linalg.norm(a - b) < 1e-5 * np.linalg.norm(b)     # (gradients of convolutions are added up by atomics)
+
+
 def test_a_head_and_its_layer_trained_together():
     """The operators as a program uses them: features from a hidden layer, the loss of a head over many classes, its gradients,
     orthogonalised updates of both weights.  Every step's gradients are those of the formulas in 64 bits for its weights."""
