@@ -2968,12 +2968,23 @@ static void muon_groups(const Plan& P, std::vector<MuonGroup>* groups, std::vect
     }
   }
 }
+// The groups of a module in turn on its stream and on those of its weight gradients (their chains of small products do not fill
+// the machine: ResNet-50 1.27 ms a step on one stream a module, see lp_step_muon); each stream has a part of the scratch.
+static std::vector<size_t> muon_lanes(const Plan& P, const std::vector<MuonGroup>& groups, bool split) {
+  std::vector<size_t> bytes(1 + P.side.size(), 0);
+  for (size_t i = 0; i < groups.size(); ++i) {
+    const MuonGroup& g = groups[i];
+    size_t& b = bytes[i % bytes.size()];
+    b = std::max(b, ortho_scratch_bytes((int)g.off.size(), g.rows, g.cols, split));
+  }
+  return bytes;
+}
 static size_t muon_module_scratch(const Plan& P, bool split) {
   std::vector<MuonGroup> groups;
   muon_groups(P, &groups, nullptr);
-  size_t most = 0;
-  for (const MuonGroup& g : groups) most = std::max(most, ortho_scratch_bytes((int)g.off.size(), g.rows, g.cols, split));
-  return most;
+  size_t total = 0;
+  for (size_t b : muon_lanes(P, groups, split)) total += b;
+  return total;
 }
 
 size_t lp_step_muon_scratch_bytes(lp_handle* h) {
@@ -2988,7 +2999,7 @@ size_t lp_step_muon_scratch_bytes(lp_handle* h) {
 }
 
 static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momentum, bool nesterov, float weight_decay, float kappa_step,
-                       void* lambda_inout, void* scratch, cudaStream_t st) try {
+                       void* lambda_inout, void* scratch, cudaStream_t st, bool apart) try {
   Plan& P = h->modules[k];
   const bool kappa = lambda_inout && k + 1 < h->net.K;
   TimelineScope ts(h, st, k, LP_OP_UPDATE, LP_PHASE_UPDATE, (momentum != 0.f ? 20.0 : 12.0) * (double)P.ps.n +
@@ -2996,7 +3007,21 @@ static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momen
   std::vector<MuonGroup> groups;
   std::vector<SgdSpans> spans;
   muon_groups(P, &groups, &spans);
-  for (const MuonGroup& g : groups) {
+  const std::vector<size_t> bytes = muon_lanes(P, groups, h->dtype == LP_F32);
+  const size_t lanes = bytes.size();
+  apart = apart && lanes > 1 && groups.size() > 1 && can_fork(st, P.side);
+  if (apart) LP_CUDA_OK(cudaEventRecord(P.side_ev[0], st));
+  int rc = LP_OK;
+  size_t forked = 0;
+  uint8_t* at = (uint8_t*)scratch;
+  for (size_t i = 0; i < groups.size() && rc == LP_OK; ++i) {
+    const MuonGroup& g = groups[i];
+    const size_t lane = i % lanes;
+    if (lane == 0) at = (uint8_t*)scratch;
+    if (apart && lane > forked) {
+      if (cudaStreamWaitEvent(P.side[lane - 1], P.side_ev[0], 0) != cudaSuccess) { rc = LP_ERR_CUDA; break; }
+      forked = lane;
+    }
     OrthoProblem q;
     memset(&q, 0, sizeof(q));
     q.batch = (int)g.off.size(); q.rows = g.rows; q.cols = g.cols;
@@ -3010,10 +3035,14 @@ static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momen
     q.step = -lr_conv * sqrtf(std::max(1.f, (float)g.rows / (float)g.cols));
     q.err = h->dev_err;
     long long n = 0;
-    const int rc = ortho_run(q, scratch, st, &n);
+    rc = ortho_run(q, at, apart && lane ? P.side[lane - 1] : st, &n);
+    at += bytes[lane];
     h->launches += n;
-    if (rc != LP_OK) return rc;
   }
+  for (size_t l = forked; l-- > 0;)   // (joined whatever happened)
+    if (cudaEventRecord(P.side_done[l], P.side[l]) != cudaSuccess || cudaStreamWaitEvent(st, P.side_done[l], 0) != cudaSuccess)
+      if (rc == LP_OK) rc = LP_ERR_CUDA;
+  if (rc != LP_OK) return rc;
   for (const SgdSpans& s : spans) {
     int most = 0;
     for (int i = 0; i < s.n; ++i) most = std::max(most, s.span[i].count);
@@ -3022,7 +3051,7 @@ static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momen
     h->launches++;
     LP_CUDA_OK(cudaGetLastError());
   }
-  const int rc = pack_weights(h, P, st);
+  rc = pack_weights(h, P, st);
   if (rc != LP_OK) return rc;
   P.ps.grads_fresh = false;
   return kappa ? update_kappa(h, k, kappa_step, lambda_inout, st) : LP_OK;
@@ -3067,7 +3096,7 @@ int lp_step_muon(lp_handle* h, float lr_conv, float lr, float momentum, int nest
     }
     if (h->modules[k].ps.grads_fresh)
       first_err = muon_module(h, k, lr_conv, lr, momentum, nesterov != 0, weight_decay, kappa_step,
-                              (lambdas_inout && k + 1 < K) ? lambdas_inout[k] : nullptr, at, apart ? h->streams[k] : st);
+                              (lambdas_inout && k + 1 < K) ? lambdas_inout[k] : nullptr, at, apart ? h->streams[k] : st, apart);
     at += sizes[k];
   }
   for (int k = 0; k < forked; ++k)
