@@ -65,7 +65,9 @@ static int gemm_init_dev() {
   if ((rc = gemm_set_attributes<EPI_H16, GEMM_ONE>()) != LP_OK || (rc = gemm_set_attributes<EPI_H16, GEMM_LOW>()) != LP_OK ||
       (rc = gemm_set_attributes<EPI_H16, GEMM_SPLIT>()) != LP_OK || (rc = gemm_set_attributes<EPI_OUT, GEMM_ONE>()) != LP_OK ||
       (rc = gemm_set_attributes<EPI_OUT, GEMM_LOW>()) != LP_OK || (rc = gemm_set_attributes<EPI_OUT, GEMM_SPLIT>()) != LP_OK ||
-      (rc = gemm_set_attributes<EPI_CE, GEMM_ONE>()) != LP_OK || (rc = gemm_set_attributes<EPI_CE, GEMM_SPLIT>()) != LP_OK)
+      (rc = gemm_set_attributes<EPI_CE, GEMM_ONE>()) != LP_OK || (rc = gemm_set_attributes<EPI_CE, GEMM_SPLIT>()) != LP_OK ||
+      (rc = gemm_set_attributes<EPI_CE, GEMM_LONG>()) != LP_OK || (rc = gemm_set_attributes<EPI_H16, GEMM_LONG>()) != LP_OK ||
+      (rc = gemm_set_attributes<EPI_OUT, GEMM_LONG>()) != LP_OK)
     return rc;
   D.gemm_pairs = max_clusters(2, gemm_tc_kernel<EPI_OUT, GEMM_PAIR, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
   for (int c = 2; c <= 4; ++c) 
@@ -133,7 +135,9 @@ static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bo
   p.total_tiles = (int)(per * p.batch);
   p.group_m = std::min(p.tiles_m, pair ? 8 : 16);
   p.kblocks = (int)((K + 63) / 64);
-  if (!p.round_len) p.round_len = 1;
+  // K blocks an accumulation: one where fp32 results are wanted; else as many as cost a sum 2^-11 of it (2^14 steps, each cut off by
+  // 2^-25 on average)
+  if (!p.round_len) p.round_len = p.a_planes == 2 && p.b_planes == 2 ? 1 : 4096;
   p.a_mn = a_mn;
   p.b_mn = b_mn;
   // operand format: bits 7 and 10 (bf16) on top of fp32 accumulation and the shape
@@ -146,7 +150,10 @@ static int launch_gemm(tc::GemmParams& p, long long K, const CUtensorMap& ma, bo
     p.out_vec = vec;
   }
   cudaError_t e;
-  if (p.a_planes == 1 && p.b_planes == 1) e = start_gemm<kEpi, tc::GEMM_ONE>(p, ma, mb, cut, st);
+  if (p.a_planes == 1 && p.b_planes == 1) {
+    if (p.kblocks > p.round_len) e = start_gemm<kEpi, tc::GEMM_LONG>(p, ma, mb, cut, st);
+    else e = start_gemm<kEpi, tc::GEMM_ONE>(p, ma, mb, cut, st);
+  }
   else if (p.a_planes == 2 && p.b_planes == 2) e = start_gemm<kEpi, tc::GEMM_SPLIT>(p, ma, mb, cut, st);
   else if constexpr (kEpi != tc::EPI_CE) e = start_gemm<kEpi, tc::GEMM_LOW>(p, ma, mb, cut, st);
   else return LP_ERR_UNSUPPORTED;

@@ -55,7 +55,7 @@ struct GemmParams {
   int group_m;                    // row tiles that are walked together (they share B tiles in L2)
   int kblocks;
   int a_planes, b_planes;         // parts of each operand (1 or 2), `batch` matrices apart
-  int round_len;                  // kRounds: K blocks per accumulation (0: one)
+  int round_len;                  // kRounds: K blocks per accumulation (0: see launch_gemm)
   int a_mn, b_mn;                 // 1: the operand's row index is the contiguous one
   uint32_t idesc;
   // 1: the kernel before reads and writes nothing of this one's (and has itself waited for what this one reads, before it let
@@ -362,6 +362,7 @@ enum GemmMode {
   GEMM_ONE = 0,      // one plane of each operand
   GEMM_LOW = 1,      // a low part of one operand, too
   GEMM_SPLIT = 2,    // both parts of both, in rounds
+  GEMM_LONG = 3,     // one plane of each, in rounds (a long K whose sum is wanted in fp32)
 };
 
 // How a tile is computed.
@@ -425,9 +426,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   // (its share of K: at least one K block, see gemm_cut)
   const int k_first = kKSplit ? p.kblocks * (int)crank / ctas : 0;
   const int steps = kKSplit ? p.kblocks * (int)(crank + 1) / ctas - k_first : p.kblocks;
-  constexpr bool kRounds = kMode == GEMM_SPLIT;
+  constexpr bool kRounds = kMode == GEMM_SPLIT || kMode == GEMM_LONG;
   const int round_len = kRounds ? p.round_len : steps;
-  constexpr uint32_t kTiles = 2 + kMode, kStages = 12 / kTiles, kStageBytes = kTiles * kGemmTileBytes;
+  constexpr uint32_t kTiles = kMode == GEMM_SPLIT ? 4 : kMode == GEMM_LOW ? 3 : 2, kStages = 12 / kTiles, kStageBytes = kTiles * kGemmTileBytes;
   // (GEMM_LOW: which operand has two parts is known at run time)
   const int a_planes = kMode == GEMM_SPLIT ? 2 : (kMode == GEMM_LOW ? p.a_planes : 1);
   bool failed = false;

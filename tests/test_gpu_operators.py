@@ -181,7 +181,7 @@ def ortho_tol(dtype, steps=5):
 
 ORTHO_SIZES = [(1, 1, 1), (3, 1, 5), (3, 7, 1), (2, 16, 27), (5, 16, 144), (18, 64, 576), (2, 33, 31), (1, 127, 129), (1, 128, 128),
                (2, 129, 257), (1, 257, 129), (3, 320, 64), (1, 640, 5760), (1, 2048, 512), (70, 24, 40), (1, 1000, 1003),
-               (2, 128, 1152), (1, 5000, 7), (200, 64, 64), (1, 100, 40000), (3, 1152, 127), (1, 17, 33), (2, 3, 3000)]
+               (2, 128, 1152), (1, 5000, 7), (1, 2, 6000000), (1, 1500000, 3), (200, 64, 64), (1, 100, 40000), (3, 1152, 127), (1, 17, 33), (2, 3, 3000)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -236,6 +236,20 @@ def test_rows_that_do_not_count_reach_nothing(dtype, T):
     if T == 1:   # no row counts: the loss and the gradients are zeros
         assert float(got["loss"][0]) == 0 and float(alone["loss"][0]) == 0
         assert all(not bool(got[k].any()) for k in ("dx", "dw", "dbias"))
+
+
+@pytest.mark.parametrize("T", [20, 300])
+def test_long_sums_are_added_up_in_fp32(T):
+    """20000 features: 1250 steps of the tensor cores, each of which cuts the sum off (2^-24 of it at most, half of that on
+    average and always towards zero).  Rounds of 256 steps are added up apart: 2^-25 * 256 = 7.6e-6 of a logit at most, and half
+    of that where the sum grows evenly; the loss is a difference of logits of its own size."""
+    D, V = 20000, 300
+    x, w, b, labels = ce_inputs(T, D, V, "bf16")
+    ref = ce_reference(x, w, b, labels)
+    got = ce_run(x, w, b, labels)
+    ce_check(got, ref, "bf16", D, V, T)
+    err = (got["row_loss"].double() - ref["row_loss"]).abs()
+    assert bool((err <= 2.0 ** -25 * 256 * 2 * ref["l"].abs().amax(1) + 8 * EPS32 * (1 + ref["lse"].abs())).all())
 
 
 @pytest.mark.parametrize("T", [2, 40])
