@@ -70,7 +70,7 @@ static int gemm_init_dev() {
       (rc = gemm_set_attributes<EPI_OUT, GEMM_LONG>()) != LP_OK)
     return rc;
   D.gemm_pairs = max_clusters(2, gemm_tc_kernel<EPI_OUT, GEMM_PAIR, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
-  for (int c = 2; c <= 4; ++c) 
+  for (int c = 2; c <= 4; ++c)
     D.gemm_clusters[c] = max_clusters(c, gemm_tc_kernel<EPI_OUT, GEMM_KSPLIT, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
   D.gemm_attr = true;
   return LP_OK;
@@ -102,7 +102,7 @@ static GemmCut gemm_cut(long long M, long long N, long long K, int batch, bool s
     const long long t = (kb + 2) * c_pair * waves(count(256), D.gemm_pairs);
     if (t <= time) { best = GemmCut{tc::GEMM_PAIR, 2}; time = t; }
   }
-    for (int c = 2; c <= 4 && c <= kb; ++c) {
+  for (int c = 2; c <= 4 && c <= kb; ++c) {
     if (D.gemm_clusters[c] < 1) continue;
     const long long t = (((kb + c - 1) / c + 2) * c_single + 2000) * waves(count(128), D.gemm_clusters[c]);
     if (t < time) { best = GemmCut{tc::GEMM_KSPLIT, c}; time = t; }

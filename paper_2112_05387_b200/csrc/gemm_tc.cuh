@@ -134,9 +134,6 @@ __device__ __forceinline__ void half2_floats(uint32_t u, float& a, float& b) {
   a = f.x;
   b = f.y;
 }
-__device__ __forceinline__ uint32_t pack_half2(__half a, __half b) {
-  return (uint32_t)__half_as_ushort(a) | ((uint32_t)__half_as_ushort(b) << 16);
-}
 // Two at once (one instruction; converting one value at a time runs at an eighth of the rate).
 __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
@@ -351,6 +348,15 @@ __device__ __forceinline__ void ce_logits(const GemmParams& p, int col, float f,
 __device__ __forceinline__ float ce_bias(const GemmParams& p, int col) {
   if (!p.bias || col >= p.N) return 0.f;
   return p.bias_bf16 ? __bfloat162float(((const bf16*)p.bias)[col]) : ((const float*)p.bias)[col];
+}
+
+// bias[g], in registers
+template <int N>
+__device__ __forceinline__ float ce_pick(const float (&bias)[N], int g) {
+  float v = bias[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) v = g == i ? bias[i] : v;
+  return v;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -638,7 +644,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         for (int g = 0; g < groups; ++g) {
           float v[32];
           tmem_ld32(taddr + g * 32, v);
-          ce_logits(p, col0 + g * 32, f, g == 0 ? bias[0] : g == 1 ? bias[1] : g == 2 ? bias[kGroups > 2 ? 2 : 0] : bias[kGroups > 2 ? 3 : 0], v);
+          ce_logits(p, col0 + g * 32, f, ce_pick(bias, g), v);
 #pragma unroll
           for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
         }
@@ -650,7 +656,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           float v[32];
           tmem_ld32(taddr + g * 32, v);
           if (g + 1 == groups) release();
-          ce_logits(p, col, f, g == 0 ? bias[0] : g == 1 ? bias[1] : g == 2 ? bias[kGroups > 2 ? 2 : 0] : bias[kGroups > 2 ? 3 : 0], v);
+          ce_logits(p, col, f, ce_pick(bias, g), v);
           if (label >= col && label < col + 32) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)

@@ -26,21 +26,10 @@ struct CeHeader {
   int count;          // rows whose label is a class
   float logit_f;      // scale of x w^T's accumulator
   float dx_f, dw_f;   // scales of the gradients' accumulators
-  float x_scale, w_scale;
   float grad_f;       // g / count
 };
 
 __device__ __forceinline__ bool ce_counts(int label, int V) { return label >= 0 && label < V; }
-
-__device__ __forceinline__ float block_sum(float v, float* part) {
-  v = warp_sum(v);
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-  __syncthreads();
-  float s = 0.f;
-  for (int i = 0; i < kCeThreads / 32; ++i) s += part[i];
-  __syncthreads();
-  return s;
-}
 
 // Number of rows that count, by one block; to thread 0.
 __device__ __forceinline__ int ce_count_rows(const int32_t* labels, int T, int V) {
@@ -76,13 +65,18 @@ ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int V, const float*
   const float* v = of_w ? w : x;
   const long long n = of_w ? nw : nx;
   const int k = of_w ? b - parts : b;
-  const long long lo = n * k / parts, hi = n * (k + 1) / parts;
+  const long long lo = n / 4 * k / parts, hi = n / 4 * (k + 1) / parts;
   float m = 0.f;
+  auto take = [&](float a) {
+    if (fabsf(a) <= 3.4028235e38f) m = fmaxf(m, fabsf(a));
+  };
 #pragma unroll 4
   for (long long i = lo + threadIdx.x; i < hi; i += kCeThreads) {
-    const float a = fabsf(v[i]);
-    if (a <= 3.4028235e38f) m = fmaxf(m, a);
+    float f[4];
+    ldv(v + 4 * i, f);
+    for (int j = 0; j < 4; ++j) take(f[j]);
   }
+  if (k == 0 && threadIdx.x < n % 4) take(v[n - 1 - threadIdx.x]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
@@ -102,8 +96,8 @@ __device__ __forceinline__ float ce_scale_of(float amax) {
 
 // The operands as the products take them, rows `ld` apart: fp32 as fp16 high and low parts of the scaled values, bf16 as it is.
 // Rows of x whose label is no class become zeros: what stands there (padding, NaN) must not reach dw through a product with 0.
-// Blocks [1, xb) take x, the rest w (none where it is used in place), block 0 nothing but the header (bf16 problems: the count of rows with it).  kVec: D is a
-// multiple of 8.
+// Blocks [1, xb) take x, the rest w (none where it is used in place), block 0 nothing but the header (bf16 problems: the count of
+// rows with it).  kVec: D is a multiple of 8.
 template <bool kVec>
 __global__ void __launch_bounds__(kCeThreads)
 ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int32_t* __restrict__ labels, int is_bf16, int T, int D, int V,
@@ -131,8 +125,6 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int
     }
     const float gf = counted > 0 ? g / (float)counted : 0.f;
     const float dl = is_bf16 ? 1.f : 1.f / kCeDlScale;
-    hdr->x_scale = scales[0];
-    hdr->w_scale = scales[1];
     hdr->logit_f = (1.f / scales[0]) * (1.f / scales[1]);
     hdr->grad_f = gf;
     hdr->dx_f = gf * dl * (1.f / scales[1]);

@@ -430,8 +430,8 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   if (s.x) {
     const int xb = 1 + grid_for((long long)T * D, kCeThreads * 8, Dv.sm_count, 4);
     const int wb = s.w ? grid_for((long long)V * D, kCeThreads * 8, Dv.sm_count, 8) : 0;
-    LP_CUDA_OK(launch_pdl(D % 8 ? ce_pack_kernel<false> : ce_pack_kernel<true>, dim3(xb + wb), dim3(kCeThreads), 0, st, x, w, labels, is_bf16, T, D, V, s.ld_d, s.x, x_plane, s.w,
-                          w_plane, xb, (const float*)s.amax, kCeAmaxParts, grad_scale, s.hdr));
+    LP_CUDA_OK(launch_pdl(D % 8 ? ce_pack_kernel<false> : ce_pack_kernel<true>, dim3(xb + wb), dim3(kCeThreads), 0, st, x, w, labels, is_bf16, T,
+                          D, V, s.ld_d, s.x, x_plane, s.w, w_plane, xb, (const float*)s.amax, kCeAmaxParts, grad_scale, s.hdr));
   }
   const void* xm = s.x ? (const void*)s.x : x;
   const void* wm = s.w ? (const void*)s.w : w;
