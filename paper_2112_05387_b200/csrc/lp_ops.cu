@@ -258,7 +258,9 @@ static int check_ortho(int dtype, int batch, int rows, int cols, int steps, floa
 // one piece.
 static const size_t kCePieceBytes = (size_t)512 << 20;
 static const int kCeAmaxParts = 592;
-static const int kCeRound = 4;              // K blocks an accumulation (fp32 problems): 2e-7 to 6e-7 of a gradient
+// K blocks an accumulation (fp32 problems).  Four: 3e-7 to 9e-7 of a gradient, 1001 x 640 x 20011 339 us (two: 354, one: 371); two
+// where K is shared and short, 2e-7 to 4e-7, at no cost that shows.
+static int ce_round(const GemmCut& cut, long long K) { return cut.kind == tc::GEMM_KSPLIT && K <= 4096 ? 2 : 4; }
 static const int kCeLongRound = 64;         // and of bf16 logits: each of its 256 steps is cut off, 4096 features 1e-6 of the loss
 static const int kCeFewBlocks = 592;        // four an SM
 static const size_t kCeFewSmem = 96 * 1024;
@@ -458,7 +460,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     p.bias = bias; p.bias_bf16 = is_bf16; p.labels = labels + r0;
     p.stats = s.stats; p.stats_ld = s.rows; p.target = s.target + r0;
     p.h_out = s.p; p.h_ld = s.ld_v; p.h_plane = s.f32 ? p_plane : 0;
-    p.round_len = s.f32 ? kCeRound : kCeLongRound;
+    p.round_len = s.f32 ? ce_round(cut, D) : kCeLongRound;
     if (!s.x && r0 == 0) p.clear = &s.hdr->err;   // (no kernel before that could have)
     if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, cut, st)) != LP_OK) return rc;
     // few rows and parts: one block does the rest of the loss
@@ -484,9 +486,10 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       memset(&p, 0, sizeof(p));
       p.M = rows; p.N = D; p.batch = 1; p.err = &s.hdr->err;
       p.a_planes = p.b_planes = planes;
-      p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1; p.round_len = s.f32 ? kCeRound : 0;
+      p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1;
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
       const GemmCut kd = gemm_cut(rows, D, V, 1, false, planes, planes);
+      p.round_len = s.f32 ? ce_round(kd, V) : 0;
       if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, kd, st)) != LP_OK) return rc;
       dx_idle = p.total_tiles * kd.ctas < Dv.sm_count;
     }
@@ -496,7 +499,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       memset(&p, 0, sizeof(p));
       p.M = V; p.N = D; p.batch = 1; p.err = &s.hdr->err;
       p.a_planes = p.b_planes = planes;
-      p.f = 1.f; p.f_dev = &s.hdr->dw_f; p.f_pow = 1; p.round_len = s.f32 ? kCeRound : 0;
+      p.f = 1.f; p.f_dev = &s.hdr->dw_f; p.f_pow = 1;
       p.out = dw; p.out_bf16 = is_bf16; p.out_ld = D;
       // (beside dx's product where that leaves SMs idle: 64 rows x 512 x 1000 30 us and 33 one after the other, fp32 43 and 48;
       // where it has all of them the two share L2 badly, 4096 x 2048 x 32000 1.32 ms and 1.31)
@@ -507,6 +510,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
         p.acc_last = r0 + rows == T;
       }
       const GemmCut kd = gemm_cut(V, D, rows, 1, false, planes, planes);
+      p.round_len = s.f32 ? ce_round(kd, rows) : 0;
       if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, kd, st)) != LP_OK) return rc;
     }
   }
