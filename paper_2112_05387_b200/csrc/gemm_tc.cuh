@@ -596,9 +596,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       }
       if constexpr (kKSplit) {
         // Group g of 32 columns is finished by CTA g % c.  Every CTA leaves the groups of the others in its own shared memory (over
-        // the ring: all its products have read it), 128 rows a column; after the barrier the warps that have the CTA's group
-        // fetch it from each of the others and add up, in the CTAs' order.
-        float* ring = reinterpret_cast<float*>(smem);
+        // the ring: all its products have read it), four columns of 128 rows together; after the barrier the warps that have the
+        // CTA's group fetch it from each of the others, 512 bytes in a row an access (16 bytes at a time from rows apart took
+        // twice as long as anything else here), and add up, in the CTAs' order.
+        float4* ring = reinterpret_cast<float4*>(smem);
         const int c = (int)cluster_nctas();
         int mine = -1;
 #pragma unroll 1
@@ -609,20 +610,22 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           } else if (!failed) {
             float v[32];
             tmem_ld32(taddr + g * 32, v);
+            float4* to = ring + grp * 8 * 128 + q * 32 + lane;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) ring[(grp * 32 + j) * 128 + q * 32 + lane] = v[j];
+            for (int j = 0; j < 8; ++j) to[j * 128] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
           }
         }
         __syncwarp();
         cluster_sync_all();
         if (failed || mine < 0) break;
         taddr += mine * 32;
-        const uint32_t from = smem_u32(ring + (half * kGroups + mine) * 32 * 128 + q * 32 + lane);
+        const uint32_t from = smem_u32(ring + (half * kGroups + mine) * 8 * 128 + q * 32 + lane);
         col0 += mine * 32;
         if (mine) bias[0] = bias[kGroups - 1];
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = 0.f;
+#pragma unroll 1
         for (int r = 0; r < c; ++r) {
           float x[32];
           if (r == (int)crank) {
@@ -630,7 +633,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           } else {
             const uint32_t at = mapa_u32(from, r);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) x[j] = ld_cluster_f32(at + j * 512);
+            for (int j = 0; j < 8; ++j) {
+              const float4 f = ld_cluster_f32x4(at + j * 2048);
+              x[4 * j] = f.x; x[4 * j + 1] = f.y; x[4 * j + 2] = f.z; x[4 * j + 3] = f.w;
+            }
           }
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] += x[j];

@@ -42,11 +42,6 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
-}
 __device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
   double v;
   asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
@@ -226,7 +221,7 @@ ortho_small_kernel(const __grid_constant__ OrthoSmall q) {
         float4 x[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r)
-          if (r < q.ctas) x[r] = ld_cluster_f32x4(tc::mapa_u32(tc::smem_u32(part + k * S * S + e), r));
+          if (r < q.ctas) x[r] = tc::ld_cluster_f32x4(tc::mapa_u32(tc::smem_u32(part + k * S * S + e), r));
 #pragma unroll
         for (int r = 0; r < 8; ++r)
           if (r < q.ctas) { v[0] += x[r].x; v[1] += x[r].y; v[2] += x[r].z; v[3] += x[r].w; }
