@@ -718,7 +718,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
   }
   if (p.wait_late) pdl_wait();
-  if constexpr (kCluster) cluster_sync_all();   // no CTA leaves while another may still signal it or read its ring
+  if constexpr (kCluster) cluster_sync_relaxed();   // no CTA leaves while another may still signal it or read its ring
   if (warp == 2) {
     tc_fence_after();
     if constexpr (kPair) tmem2_dealloc(tmem_base, kTmem);

@@ -314,6 +314,11 @@ __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_add
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The same without ordering memory accesses: before a CTA leaves whose shared memory or barriers others have used (with a release it
+// would wait there for its stores to global memory).
+__device__ __forceinline__ void cluster_sync_relaxed() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
 // TMA loads into this CTA's shared memory whose completion is counted on a barrier given by its cluster
 // address (the leader's barrier): the cta_group::2 form allows the barrier to live in the peer CTA.
 __device__ __forceinline__ void tma2_load_2d(void* dst, const CUtensorMap* map, uint32_t bar_cluster_addr, int c0, int c1) {
