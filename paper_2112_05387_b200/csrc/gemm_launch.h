@@ -84,8 +84,10 @@ struct GemmCut {
 // Whichever way has its busiest CTA finish first.  A K block of `loads` tiles of 16 KB and `products` of them takes an SM 256
 // cycles a load (64 bytes a cycle from L2) or, for each product, 512 cycles (128 x 256 of a pair's tile; 690 with one plane of
 // each operand, measured: 0.47 us with 42 pairs at work) or 256 (128 x 128).  With few tiles a cluster shares K, at the price of
-// an exchange (2000 cycles: 300 x 400, one plane, five to seven K blocks, 105 us a call without and 115 with it; two planes, 180
-// and 149); of four CTAs at most (16 K blocks over eight: 21 us, over four: 13).
+// an exchange: about 2500 cycles beside three products a K block, 4500 beside one or two, whose K blocks take less than counted
+// here while few SMs draw on L2 (us a call of five steps with 800, 2000, 3000, 4500, 6500 cycles: 300 x 400 in fp32 130, 130, 131,
+// 145, 161, 600 x 600 in bf16 126, 126, 126, 115, 116, 200 x 200 in bf16 111, 83, 80, 80, 80); of four CTAs at most (16 K blocks
+// over eight: 21 us, over four: 13).
 static GemmCut gemm_cut(long long M, long long N, long long K, int batch, bool sym, int a_planes, int b_planes) {
   const Device& D = cur_dev();
   auto count = [&](int t) {
@@ -104,7 +106,7 @@ static GemmCut gemm_cut(long long M, long long N, long long K, int batch, bool s
   }
   for (int c = 2; c <= 4 && c <= kb; ++c) {
     if (D.gemm_clusters[c] < 1) continue;
-    const long long t = (((kb + c - 1) / c + 2) * c_single + 2000) * waves(count(128), D.gemm_clusters[c]);
+    const long long t = (((kb + c - 1) / c + 2) * c_single + (products == 3 ? 2500 : 4500)) * waves(count(128), D.gemm_clusters[c]);
     if (t < time) { best = GemmCut{tc::GEMM_KSPLIT, c}; time = t; }
   }
   return best;
