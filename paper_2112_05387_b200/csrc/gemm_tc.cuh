@@ -478,6 +478,12 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         if (++s == kStages) { s = 0; ph ^= 1; }
       }
     }
+    if constexpr (kPair) {   // what the leader's products signal has arrived before this CTA leaves (the last barrier orders nothing)
+      for (uint32_t i = 0; i < kStages && !failed; ++i) {
+        failed = !mbar_wait_warp(&tail->empty[s], ph ^ 1, abort_flag);
+        if (++s == kStages) { s = 0; ph ^= 1; }
+      }
+    }
   } else if (warp == 1 && leader) {
     // one thread issues (see the MMA issuers of conv_tc_kernel)
     if (elect_one()) {
@@ -526,6 +532,13 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           if (failed) break;
           if constexpr (kPair) mma2_commit_both(&tail->tmem_full[buf]);
           else mma_commit(&tail->tmem_full[buf]);
+          buf ^= 1;
+          if (!buf) bph ^= 1;
+        }
+      }
+      if constexpr (kPair) {   // and what the other CTA's epilogue signals has arrived here
+        for (int i = 0; i < 2 && !failed; ++i) {
+          failed = !mbar_wait_hot(&tail->tmem_empty[buf], bph ^ 1, abort_flag);
           buf ^= 1;
           if (!buf) bph ^= 1;
         }

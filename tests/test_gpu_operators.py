@@ -713,6 +713,54 @@ def test_the_step_recorded_and_replayed_equals_the_calls():
         assert np.linalg.norm(a - b) < 1e-5 * np.linalg.norm(b)     # (gradients of convolutions are added up by atomics)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_single_gradients_of_rows_in_pieces(dtype):
+    """Odd rows of dw and dx over several pieces, each gradient asked for by itself: the formulas, and the same bits."""
+    import torch
+    T, D, V = 3000, 33, 100001
+    x, w, b, labels = ce_inputs(T, D, V, dtype, ignored=0.1, seed=5)
+    got = ce_run(x, w, b, labels, scale=3.0)
+    ce_check(got, ce_reference(x, w, b, labels, scale=3.0), dtype, D, V, T)
+    for want in ("dx", "dw", "dbias"):
+        one = ce_run(x, w, b, labels, scale=3.0, want=(want,))
+        assert set(one) == {"loss", "row_loss", want} and all(torch.equal(one[k], got[k]) for k in one), want
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 40, 90), (1, 200, 330), (1, 600, 900)], ids=str)
+def test_the_update_recorded_and_replayed_equals_the_calls(size, dtype):
+    """One launch, shared K, and tiles of CTA pairs; a replay sees the weights and the momentum that the one before left."""
+    import torch
+    import paper_2112_05387_b200 as lp
+    code, dt = (lp.LP_F32, torch.float32) if dtype == "f32" else (lp.LP_BF16, torch.bfloat16)
+    gen = torch.Generator("cuda").manual_seed(11)
+    g, w0 = [torch.randn(*size, generator=gen, device="cuda").to(dt) for _ in range(2)]
+    m0 = torch.randn(*size, generator=gen, device="cuda")
+    n = lp.lp_orthogonalize_scratch_bytes(code, *size)
+    buf, at, n = scratch_of(n)
+    state = []
+    for recorded in (False, True):
+        w, m, st = w0.clone(), m0.clone(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+
+        def update():
+            lp.lp_muon_update(code, *size, w, g, m, 0.02, 0.9, True, 0.1, 1.5, 5, None, 1e-7, at, n, st.cuda_stream)
+        if recorded:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=st):
+                update()
+            with torch.cuda.stream(st):
+                for _ in range(3):
+                    graph.replay()
+        else:
+            for _ in range(3):
+                update()
+        assert lp.lp_scratch_status(at, st.cuda_stream) == lp.LP_OK
+        state.append((w, m))
+    assert torch.equal(state[0][0], state[1][0]) and torch.equal(state[0][1], state[1][1]) and not torch.equal(state[0][0], w0)
+    del buf
+
+
 def test_a_head_and_its_layer_trained_together():
     """The operators as a program uses them: features from a hidden layer, the loss of a head over many classes, its gradients,
     orthogonalised updates of both weights.  Every step's gradients are those of the formulas in 64 bits for its weights."""
