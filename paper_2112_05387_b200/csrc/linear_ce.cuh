@@ -362,6 +362,9 @@ ce_few_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __restr
 // Exponentials -> dl (without the factor g / count), in place, and the column sums of a slab of rows for dbias: the block's slab in
 // `sums`, or dbias itself where one slab is all there is.  A warp has 256 columns of every eighth row, a thread 8 of them;
 // `part_cols` columns share a reference in `stats`.
+// Rows are taken a few at a time, all their reads ahead of the first write (348 x 3000: 12.3 -> 10.1 us).  Many rows are bound by
+// HBM, read and written in place: 4096 x 32000 114 us, 4.6 TB/s (blocks of 512, 1024 or 2048 columns 112 to 118; the rows that the
+// product wrote last first 132).
 constexpr int kCeSlab = 64;
 template <bool kF32>
 __global__ void __launch_bounds__(kCeThreads)
@@ -376,52 +379,65 @@ ce_dl_kernel(__half* __restrict__ p, long long ld, long long plane, int rows, in
   if (col < V) {
     const float2* ref = stats + (long long)(col / part_cols) * stats_ld;
     const int r1 = min(rows, (int)(blockIdx.y + 1) * kCeSlab);
-#pragma unroll 2
-    for (int r = blockIdx.y * kCeSlab + warp; r < r1; r += 8) {
-      const int label = labels[r];
-      __half* q = p + (long long)r * ld + col;
-      float v[8];
-      const uint4 h = *reinterpret_cast<const uint4*>(q);
-      uint4 l = make_uint4(0u, 0u, 0u, 0u);
-      if constexpr (kF32) l = *reinterpret_cast<const uint4*>(q + plane);
-      if (ce_counts(label, V)) {
-        const float f = exp2f(fmaf(ref[r].x - lse[r], tc::kLog2e, -tc::kCeExpBits));
-        const uint32_t u[4] = {h.x, h.y, h.z, h.w};
+    constexpr int kBatch = kF32 ? 2 : 4;   // rows whose exponentials are on their way together
+    for (int r0 = blockIdx.y * kCeSlab + warp; r0 < r1; r0 += 8 * kBatch) {
+      uint4 hs[kBatch], ls[kF32 ? kBatch : 1];
+      int labels_r[kBatch];
+      float lses[kBatch], refs[kBatch];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tc::half2_floats(u[i], v[2 * i], v[2 * i + 1]);
-        if constexpr (kF32) {
-          const uint32_t w[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float a, b;
-            tc::half2_floats(w[i], a, b);
-            v[2 * i] += a;
-            v[2 * i + 1] += b;
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= f;
-        if (label >= col && label < col + 8) {
-          const float d = expm1f(target[r] - lse[r]);   // p - 1 without the cancellation
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (col + j == label) v[j] = d;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.f;
+      for (int k = 0; k < kBatch; ++k) {
+        const int r = min(r0 + 8 * k, r1 - 1);
+        hs[k] = *reinterpret_cast<const uint4*>(p + (long long)r * ld + col);
+        if constexpr (kF32) ls[k] = *reinterpret_cast<const uint4*>(p + plane + (long long)r * ld + col);
+        labels_r[k] = labels[r];
+        lses[k] = lse[r];
+        refs[k] = ref[r].x;
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += v[j];
-      if constexpr (kF32) {
-        uint32_t hi[4], lo[4];
+      for (int k = 0; k < kBatch; ++k) {
+        const int r = r0 + 8 * k, label = labels_r[k];
+        if (r >= r1) break;
+        __half* q = p + (long long)r * ld + col;
+        float v[8];
+        if (ce_counts(label, V)) {
+          const float f = exp2f(fmaf(refs[k] - lses[k], tc::kLog2e, -tc::kCeExpBits));
+          const uint32_t u[4] = {hs[k].x, hs[k].y, hs[k].z, hs[k].w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) tc::split_f16x2(v[2 * j] * kCeDlScale, v[2 * j + 1] * kCeDlScale, hi[j], lo[j]);
-        *reinterpret_cast<uint4*>(q) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(q + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-      } else {
-        *reinterpret_cast<uint4*>(q) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                                                  pack_bf16x2(v[6], v[7]));
+          for (int i = 0; i < 4; ++i) tc::half2_floats(u[i], v[2 * i], v[2 * i + 1]);
+          if constexpr (kF32) {
+            const uint32_t w[4] = {ls[k].x, ls[k].y, ls[k].z, ls[k].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float a, b;
+              tc::half2_floats(w[i], a, b);
+              v[2 * i] += a;
+              v[2 * i + 1] += b;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] *= f;
+          if (label >= col && label < col + 8) {
+            const float d = expm1f(target[r] - lses[k]);   // p - 1 without the cancellation
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (col + j == label) v[j] = d;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += v[j];
+        if constexpr (kF32) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) tc::split_f16x2(v[2 * j] * kCeDlScale, v[2 * j + 1] * kCeDlScale, hi[j], lo[j]);
+          *reinterpret_cast<uint4*>(q) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(q + plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        } else {
+          *reinterpret_cast<uint4*>(q) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                                    pack_bf16x2(v[6], v[7]));
+        }
       }
     }
   }
