@@ -34,7 +34,13 @@ __device__ __forceinline__ bool ce_counts(int label, int V) { return label >= 0 
 // Number of rows that count, by one block; to thread 0.
 __device__ __forceinline__ int ce_count_rows(const int32_t* labels, int T, int V) {
   int n = 0;
-  for (int t = threadIdx.x; t < T; t += kCeThreads) n += ce_counts(labels[t], V);
+  for (int t0 = threadIdx.x; t0 < T; t0 += 8 * kCeThreads) {
+    int label[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) label[k] = t0 + k * kCeThreads < T ? labels[t0 + k * kCeThreads] : -1;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) n += ce_counts(label[k], V);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
   __shared__ int cnt[kCeThreads / 32];
@@ -190,6 +196,39 @@ __device__ __forceinline__ void ce_join(float& m, float& s, const float2 v) {
   m = top;
 }
 
+// Every 32nd part of a row from `first` on, kBatch reads on their way together (left to the compiler they go one by one, 2011 rows of
+// 391 parts 18 us) and one maximum for all of them.
+template <int kBatch>
+__device__ __forceinline__ void ce_join_parts(float& m, float& s, const float2* stats, long long ld, int first, int parts) {
+#pragma unroll 1
+  for (int i = first; i < parts; i += 32 * kBatch) {
+    float2 v[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) v[k] = i + 32 * k < parts ? stats[(i + 32 * k) * ld] : make_float2(0.f, 0.f);
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) top = v[k].y == 0.f ? top : fmaxf(top, v[k].x);
+    if (s != 0.f) s *= exp2f((m - top) * tc::kLog2e);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) s += v[k].y == 0.f ? 0.f : v[k].y * exp2f((v[k].x - top) * tc::kLog2e);
+    m = top;
+  }
+}
+
+// The joined parts of a warp's lanes, to all of them.  (Both lanes of an exchange add the same two terms, the lower lane's first:
+// the same bits.)
+__device__ __forceinline__ void ce_join_warp(float& m, float& s) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float2 v = make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
+    float a = lane & o ? v.x : m, b = lane & o ? v.y : s;
+    ce_join(a, b, lane & o ? make_float2(m, s) : v);
+    m = a;
+    s = b;
+  }
+}
+
 // lse and loss of each row from its parts: 8 rows a block (64 bytes of each part), 32 threads a row.  On the last piece of the
 // rows (`loss` given) the block that finishes last takes the mean over the counted rows of all T, in the order of the rows.
 __global__ void __launch_bounds__(kCeThreads)
@@ -201,18 +240,20 @@ ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, 
   const int r = threadIdx.x & 7, y = threadIdx.x >> 3, row = blockIdx.x * 8 + r;
   float m = -INFINITY, s = 0.f;
   if (row < rows) {
-#pragma unroll 4
-    for (int i = y; i < parts; i += 32) ce_join(m, s, stats[(long long)i * stats_ld + row]);
+    ce_join_parts<8>(m, s, stats + row, stats_ld, y, parts);
   }
-  __shared__ float ms[32][8], ss[32][8];
-  ms[y][r] = m;
-  ss[y][r] = s;
+  __shared__ float ms[8][33], ss[8][33];
+  ms[r][y] = m;
+  ss[r][y] = s;
   __syncthreads();
-  if (y == 0 && row < rows) {
-    for (int i = 1; i < 32; ++i) ce_join(m, s, make_float2(ms[i][r], ss[i][r]));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = blockIdx.x * 8 + warp;   // a warp joins the parts of a row
+  m = ms[warp][lane];
+  s = ss[warp][lane];
+  ce_join_warp(m, s);
+  if (lane == 0 && t < rows) {
     const float l = m + logf(s);
-    lse[r0 + row] = l;
-    row_loss[r0 + row] = ce_counts(labels[r0 + row], V) ? l - target[r0 + row] : 0.f;
+    lse[r0 + t] = l;
+    row_loss[r0 + t] = ce_counts(labels[r0 + t], V) ? l - target[r0 + t] : 0.f;
     __threadfence();
   }
   if (!loss) return;
@@ -223,7 +264,13 @@ ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, 
   if (!last) return;
   __threadfence();
   double sum = 0.0;
-  for (int t = threadIdx.x; t < T; t += kCeThreads) sum += (double)__ldcg(row_loss + t);
+  for (int t0 = threadIdx.x; t0 < T; t0 += 8 * kCeThreads) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = t0 + k * kCeThreads < T ? __ldcg(row_loss + t0 + k * kCeThreads) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += (double)v[k];
+  }
   __shared__ double part[kCeThreads / 32];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -248,17 +295,8 @@ ce_finish_kernel(const float2* __restrict__ stats, long long stats_ld, int parts
   int count = 0;
   for (int row = warp; row < rows; row += 32) {
     float m = -INFINITY, s = 0.f;
-#pragma unroll 4
-    for (int i = lane; i < parts; i += 32) ce_join(m, s, stats[(long long)i * stats_ld + row]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float2 v = make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
-      // (both lanes of an exchange add the same two terms, the lower lane's first: the same bits)
-      float a = lane & o ? v.x : m, b = lane & o ? v.y : s;
-      ce_join(a, b, lane & o ? make_float2(m, s) : v);
-      m = a;
-      s = b;
-    }
+    ce_join_parts<4>(m, s, stats + row, stats_ld, lane, parts);
+    ce_join_warp(m, s);
     const float l = m + logf(s);
     const bool counts = ce_counts(labels[row], V);
     const float x = counts ? l - target[row] : 0.f;
