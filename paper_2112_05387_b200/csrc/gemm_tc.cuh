@@ -4,7 +4,8 @@
 //
 // Tiles.  A CTA pair (cta_group::2) computes 256 x 256: each CTA holds 128 rows of A and 128 of B's 256 rows, and every
 // tcgen05.mma reads both halves, so a 64-wide K block costs an SM 32 KB of loads for 128 x 256 x 64 products -- 64 bytes a
-// cycle, what an SM draws from L2.  Products with too few such tiles to fill the SMs take 128 x 128 tiles on single CTAs.
+// cycle, what an SM draws from L2.  Products with too few such tiles to fill the SMs take 128 x 128 tiles on single CTAs, and
+// products in two parts where it leaves fewer SMs idle 256 x 128 tiles on pairs.
 // The grid is persistent: a CTA (pair) walks the tiles, six stages of operands in flight, two accumulators in tensor
 // memory, so that a tile's epilogue runs under the next tile's products.
 //
@@ -376,6 +377,7 @@ enum GemmKind {
   GEMM_SINGLE = 0,   // 128 x 128 by one CTA
   GEMM_PAIR = 1,     // 256 x 256 by a CTA pair
   GEMM_KSPLIT = 2,   // 128 x 128 by a cluster of two to four CTAs, a share of K each; one tile a cluster
+  GEMM_HALF = 3,     // 256 x 128 by a CTA pair (GEMM_SPLIT: with three products a K block its loads keep up)
 };
 
 template <int kEpi, int kKind, int kMode>
@@ -387,10 +389,12 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   GemmTail* tail = reinterpret_cast<GemmTail*>(scratch_all + kGemmEpiWarps * kGemmScratchFloats);
   volatile int* abort_flag = &tail->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr bool kPair = kKind == GEMM_PAIR, kKSplit = kKind == GEMM_KSPLIT;
+  constexpr bool kHalf = kKind == GEMM_HALF, kPair = kKind == GEMM_PAIR || kHalf, kKSplit = kKind == GEMM_KSPLIT;
+  static_assert(!kHalf || kMode == GEMM_SPLIT, "stages below");
   constexpr int kCtas = kPair ? 2 : 1;
   constexpr bool kCluster = kPair || kKSplit;
-  constexpr int kTileM = 128 * kCtas, kTileN = 128 * kCtas;
+  constexpr int kTileM = 128 * kCtas, kTileN = kHalf ? 128 : 128 * kCtas;
+  constexpr uint32_t kRowsB = kTileN / kCtas, kTileBytesB = kRowsB * 128;   // of B, of a plane in a stage
   constexpr uint32_t kAccCols = kTileN, kTmem = 2 * kAccCols;
   const uint32_t crank = kCluster ? cluster_ctarank() : 0;
   const uint32_t rank = kPair ? crank : 0;      // of the CTAs that share a tile's rows
@@ -434,7 +438,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int steps = kKSplit ? p.kblocks * (int)(crank + 1) / ctas - k_first : p.kblocks;
   constexpr bool kRounds = kMode == GEMM_SPLIT || kMode == GEMM_LONG;
   const int round_len = kRounds ? p.round_len : steps;
-  constexpr uint32_t kTiles = kMode == GEMM_SPLIT ? 4 : kMode == GEMM_LOW ? 3 : 2, kStages = 12 / kTiles, kStageBytes = kTiles * kGemmTileBytes;
+  constexpr uint32_t kTiles = kMode == GEMM_SPLIT ? 4 : kMode == GEMM_LOW ? 3 : 2, kStages = kHalf ? 4 : 12 / kTiles, kStageBytes = kHalf ? 2 * (kGemmTileBytes + kTileBytesB) : kTiles * kGemmTileBytes;
+  static_assert(kStages <= kGemmStages && kStages * kStageBytes <= kGemmRingBytes, "the ring");
   // (GEMM_LOW: which operand has two parts is known at run time)
   const int a_planes = kMode == GEMM_SPLIT ? 2 : (kMode == GEMM_LOW ? p.a_planes : 1);
   bool failed = false;
@@ -444,7 +449,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     for (int t = unit; t < p.total_tiles && !failed; t += units) {
       int b, tm, tn;
       gemm_tile(p, t, b, tm, tn);
-      const int m0 = tm * kTileM + (int)rank * 128, n0 = tn * kTileN + (int)rank * 128;
+      const int m0 = tm * kTileM + (int)rank * 128, n0 = tn * kTileN + (int)(rank * kRowsB);
       for (int i = 0; i < steps; ++i) {
         if (!mbar_wait_warp(&tail->empty[s], ph ^ 1, abort_flag)) { failed = true; break; }
         if (elect_one()) {
@@ -458,11 +463,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             const bool is_a = x < a_planes;
             const CUtensorMap* map = is_a ? &tmA : &tmB;
             const int r0 = is_a ? m0 : n0, z = (is_a ? x : x - a_planes) * p.batch + b;
-            // rows contiguous: two boxes of 64 rows by 64 K; K contiguous: one of 128 rows
+            // rows contiguous: boxes of 64 rows by 64 K; K contiguous: one of all rows
             if (is_a ? p.a_mn : p.b_mn) {
               if constexpr (kPair) {
                 tma2_load_3d(dst, map, fb, r0, k0, z);
-                tma2_load_3d(dst + 8192, map, fb, r0 + 64, k0, z);
+                if (is_a || !kHalf) tma2_load_3d(dst + 8192, map, fb, r0 + 64, k0, z);
               } else {
                 tma_load_3d(dst, map, full, r0, k0, z);
                 tma_load_3d(dst + 8192, map, full, r0 + 64, k0, z);
@@ -471,7 +476,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
               if constexpr (kPair) tma2_load_3d(dst, map, fb, k0, r0, z);
               else tma_load_3d(dst, map, full, k0, r0, z);
             }
-            dst += kGemmTileBytes;
+            dst += is_a ? kGemmTileBytes : kTileBytesB;
           }
         }
         __syncwarp();
@@ -506,7 +511,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             tc_fence_after();
             const uint32_t at = base + s * kStageBytes;
             auto product = [&](int x, int y, uint32_t more) {   // tiles x (of A) and y (of B) of the stage
-              const uint64_t ad = smem_desc(da, at + x * kGemmTileBytes), bd = smem_desc(db, at + y * kGemmTileBytes);
+              const uint64_t ad = smem_desc(da, at + x * kGemmTileBytes), bd = smem_desc(db, at + (kHalf ? 2 * kGemmTileBytes + (y - 2) * kTileBytesB : y * kGemmTileBytes));
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 if constexpr (kPair) mma2_bf16(d, ad + (uint64_t)(j * ka), bd + (uint64_t)(j * kb16), p.idesc, j ? 1u : more);

@@ -172,7 +172,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   n += 2;
 
   // tensor maps, once a call: X in both buffers and both orders, A and B with K contiguous (they are symmetric)
-  CUtensorMap m_xk[2], m_xm[2], m_a, m_b;
+  CUtensorMap m_xk[2], m_xm[2], m_a, m_b, m_bh;
   for (int i = 0; i < 2; ++i) {
     const GemmOperand x{s.x[i], q.cols, q.rows, s.ld, x_mat, 2 * B, false};
     if ((rc = encode_gemm_map(&m_xk[i], x, false)) != LP_OK) return rc;
@@ -180,6 +180,9 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
   }
   if ((rc = encode_gemm_map(&m_a, GemmOperand{s.a, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
   if ((rc = encode_gemm_map(&m_b, GemmOperand{s.b, small, small, s.ld_s, s_mat, planes * B, false}, false)) != LP_OK) return rc;
+  // (B as the second operand of 256 x 128 tiles)
+  const GemmOperand b_half{s.b, small, small, s.ld_s, s_mat, planes * B, false};
+  if (tall && q.split && (rc = encode_gemm_map(&m_bh, b_half, false, rows_b(GemmCut{tc::GEMM_HALF, 2}))) != LP_OK) return rc;
   const GemmCut cut_g = gemm_cut(small, small, tall ? q.rows : q.cols, B, true, planes, planes),
                      cut_a = gemm_cut(small, small, small, B, true, planes, planes);
 
@@ -217,7 +220,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.f_dev = s.alpha; p.f_pow = first ? 1 : 0;
     const GemmCut cut_x = gemm_cut(q.rows, q.cols, small, B, false, p.a_planes, p.b_planes);
     const CUtensorMap& ma = tall ? m_xk[cur] : m_b;
-    const CUtensorMap& mb = tall ? m_b : m_xm[cur];
+    const CUtensorMap& mb = !tall ? m_xm[cur] : cut_x.kind == tc::GEMM_HALF ? m_bh : m_b;
     if (last) {
       p.out = q.out; p.out_bf16 = q.out_bf16; p.out_ld = q.cols; p.out_batch = src.elems;
       p.update = q.update; p.keep = q.keep; p.step = q.step;
@@ -440,7 +443,6 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
   const long long ldx = s.x ? s.ld_d : D, ldw = s.w ? s.ld_d : D;
   CUtensorMap m_wk, m_wm;
   const GemmOperand ow{wm, D, V, ldw, w_plane, planes, !s.f32};
-  if ((rc = encode_gemm_map(&m_wk, ow, false)) != LP_OK) return rc;
   if ((rc = encode_gemm_map(&m_wm, ow, true)) != LP_OK) return rc;
   int slab0 = 0;
   bool one_slab = false;
@@ -450,7 +452,8 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     CUtensorMap m_xk, m_xm, m_pk, m_pm;
     if ((rc = encode_gemm_map(&m_xk, ox, false)) != LP_OK) return rc;
     const GemmCut cut = gemm_cut(rows, V, D, 1, false, planes, planes);
-    const int part_cols = cut.kind == tc::GEMM_PAIR ? 128 : cut.kind == tc::GEMM_SINGLE ? 64 : 32;
+    if ((rc = encode_gemm_map(&m_wk, ow, false, rows_b(cut))) != LP_OK) return rc;
+    const int part_cols = cut.kind == tc::GEMM_PAIR ? 128 : cut.kind == tc::GEMM_KSPLIT ? 32 : 64;
     const int parts = (V + part_cols - 1) / part_cols;
     tc::GemmParams p;
     memset(&p, 0, sizeof(p));
