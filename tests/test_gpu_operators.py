@@ -761,6 +761,16 @@ def test_the_update_recorded_and_replayed_equals_the_calls(size, dtype):
     del buf
 
 
+@pytest.mark.parametrize("size", [(3, 1, 5), (7, 2, 3), (40, 3, 40), (9, 4, 100), (1, 16, 144), (2, 32, 4000), (1, 1000, 63), (40, 48, 2000)], ids=str)
+def test_few_singular_values_in_bf16_cost_one_rounding(size):
+    """With y before the rounding off by d from the formula's r: |rn(y) - r| <= |rn(y) - y| + d <= |rn(r) - y| + d <= |rn(r) - r| + 2 d,
+    where d is the bound of LP_F32."""
+    import torch
+    g = torch.randn(*size, generator=torch.Generator("cuda").manual_seed(3), device="cuda").bfloat16()
+    out, ref = ortho_run(g).double(), ortho_reference(g)
+    assert float((out - ref).norm()) <= float((ref.bfloat16().double() - ref).norm()) + 2 * ortho_tol("f32") * float(ref.norm())
+
+
 def test_a_head_and_its_layer_trained_together():
     """The operators as a program uses them: features from a hidden layer, the loss of a head over many classes, its gradients,
     orthogonalised updates of both weights.  Every step's gradients are those of the formulas in 64 bits for its weights."""
