@@ -39,7 +39,7 @@ struct Device {
   int max_pairs = 0;   // CTA pairs of conv_tc2_kernel that can be resident at once (0: not usable)
   int gemm_pairs = 0;  // the same for gemm_tc_kernel
   int small_clusters[9] = {0}; // clusters of 1, 2, 4, 8 CTAs of ortho_small_kernel
-  int gemm_clusters[5] = {0};  // and its clusters of 2 to 4 CTAs that share K
+  int gemm_clusters[9] = {0};  // and its clusters of 2 to 8 CTAs that share K
   int init() {
     if (ready) return LP_OK;
     int dev = 0;

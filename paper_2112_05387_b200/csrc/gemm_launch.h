@@ -73,7 +73,7 @@ static int gemm_init_dev() {
       (rc = gemm_set_attributes<EPI_OUT, GEMM_LONG>()) != LP_OK)
     return rc;
   D.gemm_pairs = max_clusters(2, gemm_tc_kernel<EPI_OUT, GEMM_PAIR, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
-  for (int c = 2; c <= 4; ++c)
+  for (int c = 2; c <= 8; ++c)
     D.gemm_clusters[c] = max_clusters(c, gemm_tc_kernel<EPI_OUT, GEMM_KSPLIT, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
   D.gemm_attr = true;
   return LP_OK;
@@ -93,7 +93,8 @@ static unsigned rows_b(const GemmCut& cut) { return cut.kind == tc::GEMM_HALF ? 
 // as long as the product.  With few tiles a cluster shares K, at the price of an exchange: about 2500 cycles beside three products
 // a K block, 4500 beside one or two, whose K blocks take less than counted here while few SMs draw on L2 (us a call of five steps
 // with 800, 2000, 3000, 4500, 6500 cycles: 300 x 400 in fp32 130, 130, 131, 145, 161, 600 x 600 in bf16 126, 126, 126, 115, 116,
-// 200 x 200 in bf16 111, 83, 80, 80, 80); of four CTAs at most (16 K blocks over eight: 21 us, over four: 13).
+// 200 x 200 in bf16 111, 83, 80, 80, 80); 3000 more among eight CTAs, four of which only give their sums away (200 x 8192 in fp32 184 us, 231 on
+// clusters of four, in bf16 122 and 131; 64 x 512 x 1000 of the fp32 loss 40.7 and 38.9).
 static GemmCut gemm_cut(long long M, long long N, long long K, int batch, bool sym, int a_planes, int b_planes) {
   const Device& D = cur_dev();
   auto count = [&](int t, int u) {
@@ -114,9 +115,9 @@ static GemmCut gemm_cut(long long M, long long N, long long K, int batch, bool s
       if (t_half < time) { best = GemmCut{tc::GEMM_HALF, 2}; time = t_half; }
     }
   }
-  for (int c = 2; c <= 4 && c <= kb; ++c) {
+  for (int c = 2; c <= 8 && c <= kb; c += c < 4 ? 1 : 4) {
     if (D.gemm_clusters[c] < 1) continue;
-    const long long t = (((kb + c - 1) / c + 2) * c_single + (products == 3 ? 2500 : 4500)) * waves(count(128, 128), D.gemm_clusters[c]);
+    const long long t = (((kb + c - 1) / c + 2) * c_single + (products == 3 ? 2500 : 4500) + (c == 8 ? 3000 : 0)) * waves(count(128, 128), D.gemm_clusters[c]);
     if (t < time) { best = GemmCut{tc::GEMM_KSPLIT, c}; time = t; }
   }
   return best;

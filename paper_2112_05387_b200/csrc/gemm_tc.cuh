@@ -376,7 +376,7 @@ enum GemmMode {
 enum GemmKind {
   GEMM_SINGLE = 0,   // 128 x 128 by one CTA
   GEMM_PAIR = 1,     // 256 x 256 by a CTA pair
-  GEMM_KSPLIT = 2,   // 128 x 128 by a cluster of two to four CTAs, a share of K each; one tile a cluster
+  GEMM_KSPLIT = 2,   // 128 x 128 by a cluster of 2, 3, 4 or 8 CTAs, a share of K each; one tile a cluster
   GEMM_HALF = 3,     // 256 x 128 by a CTA pair (GEMM_SPLIT: with three products a K block its loads keep up)
 };
 
