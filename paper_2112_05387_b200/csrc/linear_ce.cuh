@@ -51,10 +51,11 @@ __device__ __forceinline__ int ce_count_rows(const int32_t* labels, int T, int V
   return n;
 }
 
-// fp32 problems: block 0 counts the rows, the others take the largest finite magnitudes of x and w (parts of each).
+// fp32 problems: block 0 counts the rows, the others take the largest finite magnitudes of x and w (parts of each).  Rows of x that
+// do not count are left out: a large number in the padding would push the counted rows out of the scaled parts' bits.
 __global__ void __launch_bounds__(kCeThreads)
-ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int V, const float* __restrict__ x, long long nx, const float* __restrict__ w,
-                  long long nw, float* __restrict__ amax, int parts, CeHeader* __restrict__ hdr) {
+ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int D, int V, const float* __restrict__ x, const float* __restrict__ w,
+                  float* __restrict__ amax, int parts, CeHeader* __restrict__ hdr) {
   pdl_wait();
   pdl_launch_dependents();
   __shared__ float part[kCeThreads / 32];
@@ -69,20 +70,39 @@ ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int V, const float*
   const int b = blockIdx.x - 1;
   const bool of_w = b >= parts;
   const float* v = of_w ? w : x;
-  const long long n = of_w ? nw : nx;
+  const long long n = (long long)(of_w ? V : T) * D;
   const int k = of_w ? b - parts : b;
   const long long lo = n / 4 * k / parts, hi = n / 4 * (k + 1) / parts;
   float m = 0.f;
   auto take = [&](float a) {
     if (fabsf(a) <= 3.4028235e38f) m = fmaxf(m, fabsf(a));
   };
+  auto counts = [&](long long e, int cols) {   // whether the row of x of element e counts (the division as in ce_pack_kernel)
+    return ce_counts(labels[n >> 32 ? e / cols : (long long)((uint32_t)e / (uint32_t)cols)], V);
+  };
+  if (of_w || D % 4 == 0) {
+    // (an access has elements of one row)
 #pragma unroll 4
-  for (long long i = lo + threadIdx.x; i < hi; i += kCeThreads) {
-    float f[4];
-    ldv(v + 4 * i, f);
-    for (int j = 0; j < 4; ++j) take(f[j]);
+    for (long long i = lo + threadIdx.x; i < hi; i += kCeThreads) {
+      float f[4];
+      ldv(v + 4 * i, f);
+      const bool keep = of_w || counts(i, D / 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) take(keep ? f[j] : 0.f);
+    }
+  } else {
+#pragma unroll 1
+    for (long long i = lo + threadIdx.x; i < hi; i += kCeThreads) {
+      float f[4];
+      ldv(v + 4 * i, f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) take(counts(4 * i + j, D) ? f[j] : 0.f);
+    }
   }
-  if (k == 0 && threadIdx.x < n % 4) take(v[n - 1 - threadIdx.x]);
+  if (k == 0 && threadIdx.x < n % 4) {
+    const long long e = n - 1 - threadIdx.x;
+    take(of_w || counts(e, D) ? v[e] : 0.f);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;

@@ -436,8 +436,8 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     return s.f32 ? ce_few_rows(s, T, D, V, (const float*)x, (const float*)w, (const float*)bias, labels, rl, loss_out, st)
                  : ce_few_rows(s, T, D, V, (const bf16*)x, (const bf16*)w, (const bf16*)bias, labels, rl, loss_out, st);
   if (s.f32)
-    LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + 2 * kCeAmaxParts), dim3(kCeThreads), 0, st, labels, T, V, (const float*)x, (long long)T * D,
-                        (const float*)w, (long long)V * D, s.amax, kCeAmaxParts, s.hdr));
+    LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + 2 * kCeAmaxParts), dim3(kCeThreads), 0, st, labels, T, D, V, (const float*)x, (const float*)w,
+                          s.amax, kCeAmaxParts, s.hdr));
   if (s.x) {
     const int xb = 1 + grid_for((long long)T * D, kCeThreads * 8, Dv.sm_count, 4);
     const int wb = s.w ? grid_for((long long)V * D, kCeThreads * 8, Dv.sm_count, 8) : 0;

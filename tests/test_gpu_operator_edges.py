@@ -1,0 +1,29 @@
+"""GPU parity of the operators at the end of a training step where values stand that must not matter (rows that do not count,
+masked classes)."""
+import pytest
+
+from test_gpu_operators import ce_check, ce_inputs, ce_reference, ce_run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [1e8, -1e12, 1e30, 3.3e38])
+@pytest.mark.parametrize("T,D", [(3, 72), (70, 3), (71, 75), (300, 72)], ids=str)
+def test_finite_values_in_rows_that_do_not_count_reach_nothing(T, D, value, dtype):
+    """Padding may hold any finite number: the bits of a call whose padding is of the counted rows' size, and the formulas."""
+    import torch
+    V = 501
+    x, w, b, labels = ce_inputs(T, D, V, dtype)
+    out = torch.zeros(T, dtype=torch.bool, device="cuda")
+    out[::3] = True
+    out[T - 1] = True
+    labels[out] = -100
+    clean, clean_alone = ce_run(x, w, b, labels), ce_run(x, w, b, labels, grads=False)
+    x[out] = value
+    got, alone = ce_run(x, w, b, labels), ce_run(x, w, b, labels, grads=False)
+    ce_check(got, ce_reference(x, w, b, labels), dtype, D, V, T)
+    for k in got:
+        assert torch.equal(got[k], clean[k]), k
+    for k in alone:
+        assert torch.equal(alone[k], clean_alone[k]), k
