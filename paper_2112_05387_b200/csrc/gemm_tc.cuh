@@ -672,7 +672,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
           for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
         }
-        const float ref = top == -INFINITY ? 0.f : top;   // a half without any class counts nothing
+        // (a half without any class: its exponentials are 0, and `stats` says -inf, so that what they are multiplied by later is
+        // 0, too, however low the row's lse is)
+        const float ref = top == -INFINITY ? 0.f : top;
         float sum = 0.f;
 #pragma unroll 1
         for (int g = 0; g < groups; ++g) {
@@ -693,7 +695,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
           if (p.h_out && col < p.N && row0 < p.M) epi_h16(p, 0, row0, lane, col, false, v, scratch);
         }
-        if (row < p.M) p.stats[(long long)(col0 / (kKSplit ? 32 : kTileN / 2)) * p.stats_ld + row] = make_float2(ref, sum * 6.103515625e-5f);
+        if (row < p.M) p.stats[(long long)(col0 / (kKSplit ? 32 : kTileN / 2)) * p.stats_ld + row] = make_float2(top, sum * 6.103515625e-5f);
       } else {
         const bool mirror = p.sym && tm != tn;
 #pragma unroll 1

@@ -1,5 +1,5 @@
 """GPU parity of the operators at the end of a training step where values stand that must not matter (rows that do not count,
-masked classes)."""
+masked classes) and where logits are far from 0."""
 import pytest
 
 from test_gpu_operators import ce_check, ce_inputs, ce_reference, ce_run
@@ -27,3 +27,26 @@ def test_finite_values_in_rows_that_do_not_count_reach_nothing(T, D, value, dtyp
         assert torch.equal(got[k], clean[k]), k
     for k in alone:
         assert torch.equal(alone[k], clean_alone[k]), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [50, 99, 150, 1000])
+@pytest.mark.parametrize("size", [(1, 64, 700), (20, 64, 40), (20, 512, 700), (65, 64, 700), (300, 64, 40), (300, 64, 700), (300, 72, 20011),
+                                  (2000, 264, 20011)], ids=str)
+def test_masked_classes_beside_low_logits(size, shift, dtype):
+    """Whole parts of the classes masked, all others at logits around -shift: probability 0 and gradients of 0 for the masked
+    ones, the formulas for the rest.  Sizes of shared K, single tiles and tiles of pairs."""
+    import torch
+    T, D, V = size
+    keep = 8 if V == 40 else V // 4
+    x, w, b, labels = ce_inputs(T, D, V, dtype)
+    labels = labels % keep
+    b -= shift
+    b[keep:] = float("-inf")
+    ref, got = ce_reference(x, w, b, labels), ce_run(x, w, b, labels)
+    ce_check(got, dict(ref, mag_l=ref["mag_l"][:, :keep]), dtype, D, V, T)
+    assert not bool(got["dw"][keep:].any()) and not bool(got["dbias"][keep:].any())
+    # nothing left: 0 / 0
+    b[:] = float("-inf")
+    none = ce_run(x, w, b, labels)
+    assert bool(torch.isnan(none["row_loss"]).all()) and bool(torch.isnan(none["dx"]).all())
