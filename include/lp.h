@@ -389,11 +389,13 @@ int lp_conv2d_fwd_noalloc(int N, int H, int W, int Cin, int Cout, int R, int str
  *   l = x w^T + bias;  row_loss[t] = log sum_v exp l[t][v] - l[t][labels[t]];  loss = mean of row_loss over the counted rows
  * A row counts if its label is a class, 0 <= labels[t] < V; any other label leaves the row out: its row_loss and its row of dx
  * are 0 and nothing of x[t] (which may hold anything, NaN included) reaches dw or dbias.
- *   T from 1 to 2^28, V to 2^24, D to 2^20; x [T][D], w [V][D], bias [V] or NULL (entries may be -inf: that class then has probability 0), labels int32 [T]
+ *   T from 1 to 2^28, V to 2^24, D to 2^20; x [T][D], w [V][D], bias [V] or NULL, labels int32 [T]
+ *   (entries of bias may be -inf: that class then has probability 0, and its row of w may hold any finite numbers)
  *   loss_out: float[2] = { loss (0 if no row counts), number of counted rows }; row_loss: float[T] or NULL
  *   dx [T][D], dw [V][D], dbias [V]: grad_scale times the gradient of loss, any of them NULL; overwritten.  All NULL: the loss
  *     alone.
- * In LP_F32 products are taken from 22 bits of each operand, relative to the largest magnitude of the tensor.  A row whose
+ * In LP_F32 products are taken from 22 bits of each operand, relative to the largest magnitude in the rows of x that count and in
+ * the rows of w whose class is not masked by a bias of -inf.  A row whose
  * logits are all -inf has a loss and gradients of NaN, as the formula does.  The inputs are not changed; outputs must not
  * overlap inputs.  The gradients take the rows in pieces whose exponentials fit 512 MB (256 rows at least). */
 size_t lp_linear_cross_entropy_scratch_bytes(int dtype, int T, int D, int V, int grads);

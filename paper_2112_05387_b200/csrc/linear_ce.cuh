@@ -52,10 +52,11 @@ __device__ __forceinline__ int ce_count_rows(const int32_t* labels, int T, int V
 }
 
 // fp32 problems: block 0 counts the rows, the others take the largest finite magnitudes of x and w (parts of each).  Rows of x that
-// do not count are left out: a large number in the padding would push the counted rows out of the scaled parts' bits.
+// do not count and rows of w whose class is masked are left out: a large number in the padding would push the others out of the scaled
+// parts' bits.
 __global__ void __launch_bounds__(kCeThreads)
 ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int D, int V, const float* __restrict__ x, const float* __restrict__ w,
-                  float* __restrict__ amax, int parts, CeHeader* __restrict__ hdr) {
+                  const float* __restrict__ bias, float* __restrict__ amax, int parts, CeHeader* __restrict__ hdr) {
   pdl_wait();
   pdl_launch_dependents();
   __shared__ float part[kCeThreads / 32];
@@ -77,31 +78,47 @@ ce_prepare_kernel(const int32_t* __restrict__ labels, int T, int D, int V, const
   auto take = [&](float a) {
     if (fabsf(a) <= 3.4028235e38f) m = fmaxf(m, fabsf(a));
   };
-  auto counts = [&](long long e, int cols) {   // whether the row of x of element e counts (the division as in ce_pack_kernel)
-    return ce_counts(labels[n >> 32 ? e / cols : (long long)((uint32_t)e / (uint32_t)cols)], V);
+  auto row_of = [&](long long e, int cols) {   // (the division as in ce_pack_kernel)
+    return n >> 32 ? e / cols : (long long)((uint32_t)e / (uint32_t)cols);
   };
-  if (of_w || D % 4 == 0) {
+  // (one load, whichever it is: a branch around it would stand between the reads of an unrolled loop)
+  const int32_t* marks = of_w ? reinterpret_cast<const int32_t*>(bias) : labels;
+  auto keep = [&](long long row) {
+    const int32_t mark = __ldg(marks + row);
+    return of_w ? __int_as_float(mark) != -INFINITY : ce_counts(mark, V);
+  };
+  const bool all = of_w && !bias;
+  if (all || D % 4 == 0) {
     // (an access has elements of one row)
 #pragma unroll 4
     for (long long i = lo + threadIdx.x; i < hi; i += kCeThreads) {
       float f[4];
       ldv(v + 4 * i, f);
-      const bool keep = of_w || counts(i, D / 4);
+      const bool take_it = all || keep(row_of(i, D / 4));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) take(keep ? f[j] : 0.f);
+      for (int j = 0; j < 4; ++j) take(take_it ? f[j] : 0.f);
     }
   } else {
-#pragma unroll 1
+#pragma unroll 2
     for (long long i = lo + threadIdx.x; i < hi; i += kCeThreads) {
       float f[4];
       ldv(v + 4 * i, f);
+      long long r = row_of(4 * i, D);
+      bool take_it = keep(r);
+      int left = (int)((r + 1) * D - 4 * i);   // elements of the row from 4 i on
 #pragma unroll
-      for (int j = 0; j < 4; ++j) take(counts(4 * i + j, D) ? f[j] : 0.f);
+      for (int j = 0; j < 4; ++j, --left) {
+        if (left == 0) {
+          take_it = keep(++r);
+          left = D;
+        }
+        take(take_it ? f[j] : 0.f);
+      }
     }
   }
   if (k == 0 && threadIdx.x < n % 4) {
     const long long e = n - 1 - threadIdx.x;
-    take(of_w || counts(e, D) ? v[e] : 0.f);
+    take(all || keep(row_of(e, D)) ? v[e] : 0.f);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -121,13 +138,15 @@ __device__ __forceinline__ float ce_scale_of(float amax) {
 }
 
 // The operands as the products take them, rows `ld` apart: fp32 as fp16 high and low parts of the scaled values, bf16 as it is.
-// Rows of x whose label is no class become zeros: what stands there (padding, NaN) must not reach dw through a product with 0.
+// Rows of x whose label is no class become zeros: what stands there (padding, NaN) must not reach dw through a product with 0.  So do,
+// in fp32 problems, the finite values of a masked class's row of w, which the scale does not know (its logit is -inf and its dl 0,
+// whatever they are).
 // Blocks [1, xb) take x, the rest w (none where it is used in place), block 0 nothing but the header (bf16 problems: the count of
 // rows with it).  kVec: D is a multiple of 8.
 template <bool kVec>
 __global__ void __launch_bounds__(kCeThreads)
-ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int32_t* __restrict__ labels, int is_bf16, int T, int D, int V,
-               long long ld, __half* __restrict__ xo, long long x_plane, __half* __restrict__ wo, long long w_plane, int xb,
+ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const void* __restrict__ bias, const int32_t* __restrict__ labels, int is_bf16,
+               int T, int D, int V, long long ld, __half* __restrict__ xo, long long x_plane, __half* __restrict__ wo, long long w_plane, int xb,
                const float* __restrict__ amax, int parts, float g, CeHeader* __restrict__ hdr) {
   pdl_wait();
   pdl_launch_dependents();
@@ -171,6 +190,8 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int
     const long long r = n >> 32 ? i / per_row : (long long)((uint32_t)i / (uint32_t)per_row);
     const long long from = i * N, at = r * ld + (i - r * per_row) * N;
     const bool keep = of_w || ce_counts(labels[r], V);
+    const bool masked = of_w && !is_bf16 && bias && ((const float*)bias)[r] == -INFINITY;
+    auto scaled = [&](float a) { return !keep || (masked && fabsf(a) <= 3.4028235e38f) ? 0.f : a * scale; };
     if (is_bf16) {
       if constexpr (kVec) {
         uint4 v = ld_raw((const bf16*)src + from);
@@ -187,14 +208,14 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const int
         ldv((const float*)src + from + 4, z);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          tc::split_f16x2(keep ? v[2 * j] * scale : 0.f, keep ? v[2 * j + 1] * scale : 0.f, hi[j], lo[j]);
-          tc::split_f16x2(keep ? z[2 * j] * scale : 0.f, keep ? z[2 * j + 1] * scale : 0.f, hi[2 + j], lo[2 + j]);
+          tc::split_f16x2(scaled(v[2 * j]), scaled(v[2 * j + 1]), hi[j], lo[j]);
+          tc::split_f16x2(scaled(z[2 * j]), scaled(z[2 * j + 1]), hi[2 + j], lo[2 + j]);
         }
         *reinterpret_cast<uint4*>(dst + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(dst + plane + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       } else {
         __half hi, lo;
-        tc::split_half(keep ? ((const float*)src)[from] * scale : 0.f, hi, lo);
+        tc::split_half(scaled(((const float*)src)[from]), hi, lo);
         dst[at] = hi;
         dst[plane + at] = lo;
       }

@@ -437,12 +437,12 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
                  : ce_few_rows(s, T, D, V, (const bf16*)x, (const bf16*)w, (const bf16*)bias, labels, rl, loss_out, st);
   if (s.f32)
     LP_CUDA_OK(launch_pdl(ce_prepare_kernel, dim3(1 + 2 * kCeAmaxParts), dim3(kCeThreads), 0, st, labels, T, D, V, (const float*)x, (const float*)w,
-                          s.amax, kCeAmaxParts, s.hdr));
+                          (const float*)bias, s.amax, kCeAmaxParts, s.hdr));
   if (s.x) {
     const int xb = 1 + grid_for((long long)T * D, kCeThreads * 8, Dv.sm_count, 4);
     const int wb = s.w ? grid_for((long long)V * D, kCeThreads * 8, Dv.sm_count, 8) : 0;
-    LP_CUDA_OK(launch_pdl(D % 8 ? ce_pack_kernel<false> : ce_pack_kernel<true>, dim3(xb + wb), dim3(kCeThreads), 0, st, x, w, labels, is_bf16, T,
-                          D, V, s.ld_d, s.x, x_plane, s.w, w_plane, xb, (const float*)s.amax, kCeAmaxParts, grad_scale, s.hdr));
+    LP_CUDA_OK(launch_pdl(D % 8 ? ce_pack_kernel<false> : ce_pack_kernel<true>, dim3(xb + wb), dim3(kCeThreads), 0, st, x, w, bias, labels,
+                          is_bf16, T, D, V, s.ld_d, s.x, x_plane, s.w, w_plane, xb, (const float*)s.amax, kCeAmaxParts, grad_scale, s.hdr));
   }
   const void* xm = s.x ? (const void*)s.x : x;
   const void* wm = s.w ? (const void*)s.w : w;

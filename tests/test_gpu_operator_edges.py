@@ -30,6 +30,28 @@ def test_finite_values_in_rows_that_do_not_count_reach_nothing(T, D, value, dtyp
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,D", [(2, 64), (70, 75), (300, 64)], ids=str)
+def test_finite_weights_of_masked_classes_reach_nothing(T, D, dtype):
+    """Rows of w of classes whose bias is -inf (padding up to a round number of classes): any finite number gives the same bits."""
+    import torch
+    V = 700
+    x, w, b, labels = ce_inputs(T, D, V, dtype)
+    labels = labels % 451
+    b[451:] = float("-inf")
+    clean, clean_alone = ce_run(x, w, b, labels), ce_run(x, w, b, labels, grads=False)
+    w[451:] = 1e30
+    got, alone = ce_run(x, w, b, labels), ce_run(x, w, b, labels, grads=False)
+    for k in got:
+        assert torch.equal(got[k], clean[k]), k
+    for k in alone:
+        assert torch.equal(alone[k], clean_alone[k]), k
+    # what is not finite there stays in the sums, as the formula has it
+    w[600, 1] = float("nan")
+    assert bool(torch.isnan(ce_run(x, w, b, labels)["row_loss"]).all())
+    assert bool(torch.isnan(ce_run(x, w, b, labels, grads=False)["row_loss"]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shift", [50, 99, 150, 1000])
 @pytest.mark.parametrize("size", [(1, 64, 700), (20, 64, 40), (20, 512, 700), (65, 64, 700), (300, 64, 40), (300, 64, 700), (300, 72, 20011),
                                   (2000, 264, 20011)], ids=str)
