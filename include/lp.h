@@ -390,7 +390,7 @@ int lp_conv2d_fwd_noalloc(int N, int H, int W, int Cin, int Cout, int R, int str
  * A row counts if its label is a class, 0 <= labels[t] < V; any other label leaves the row out: its row_loss and its row of dx
  * are 0 and nothing of x[t] (which may hold anything, NaN included) reaches dw or dbias.
  *   T from 1 to 2^28, V to 2^24, D to 2^20; x [T][D], w [V][D], bias [V] or NULL, labels int32 [T]
- *   (entries of bias may be -inf: that class then has probability 0, and its row of w may hold any finite numbers)
+ *   (entries of bias may be -inf: that class then has probability 0, and its row of w may hold anything with which x w^T is finite)
  *   loss_out: float[2] = { loss (0 if no row counts), number of counted rows }; row_loss: float[T] or NULL
  *   dx [T][D], dw [V][D], dbias [V]: grad_scale times the gradient of loss, any of them NULL; overwritten.  All NULL: the loss
  *     alone.

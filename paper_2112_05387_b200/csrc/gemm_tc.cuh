@@ -87,7 +87,8 @@ struct GemmParams {
   // EPI_CE
   const void* bias;               // [N] in the operands' type or null
   int bias_bf16;
-  const int32_t* labels;          // [M]
+  const int32_t* labels;          // [M]; EPI_OUT: rows whose label is none of `classes` are written as zeros (or null)
+  int classes;
   float2* stats;                  // [part of the columns][M]: maximum, sum of exponentials
   long long stats_ld;
   float* target;                  // [M]: the label's logit
@@ -565,6 +566,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       // (read while the products are under way)
       float bias[kGroups] = {};
       int label = -1;
+      // (a select, not a product: what stands there may be no number)
+      bool zero_row = false;
+      if constexpr (kEpi == EPI_OUT) {
+        if (p.labels && row < p.M) {
+          label = p.labels[row];
+          zero_row = label < 0 || label >= p.classes;
+        }
+      }
       if constexpr (kEpi == EPI_CE) {
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) bias[g] = ce_bias(p, col0 + g * 32 + lane);
@@ -706,7 +715,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           if (g + 1 == groups) release();
           if (col >= p.N || row0 >= p.M) continue;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] *= f;
+          for (int j = 0; j < 32; ++j) v[j] = zero_row ? 0.f : v[j] * f;
           if constexpr (kEpi == EPI_H16) epi_h16(p, b, row0, lane, col, mirror, v, scratch);
           else if (p.out_vec) epi_out_vec(p, b, row, col, v);
           else epi_out_any(p, b, row0, col, v, scratch, lane);

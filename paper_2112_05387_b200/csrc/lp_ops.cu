@@ -497,6 +497,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.a_planes = p.b_planes = planes;
       p.f = 1.f; p.f_dev = &s.hdr->dx_f; p.f_pow = 1;
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
+      p.labels = labels + r0; p.classes = V;   // (0 * inf of w must not reach a row that does not count)
       const GemmCut kd = gemm_cut(rows, D, V, 1, false, planes, planes);
       p.round_len = s.f32 ? ce_round(kd, V) : 0;
       if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, kd, st)) != LP_OK) return rc;

@@ -72,3 +72,22 @@ def test_masked_classes_beside_low_logits(size, shift, dtype):
     b[:] = float("-inf")
     none = ce_run(x, w, b, labels)
     assert bool(torch.isnan(none["row_loss"]).all()) and bool(torch.isnan(none["dx"]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1, 64, 700), (20, 33, 700), (70, 64, 501), (300, 64, 5003), (700, 264, 20011)], ids=str)
+def test_rows_that_do_not_count_beside_infinite_weights(size, dtype):
+    """Their rows of dx and their losses are 0, whatever w holds; the counted rows' are NaN, as the formulas have it."""
+    import torch
+    T, D, V = size
+    x, w, b, labels = ce_inputs(T, D, V, dtype)
+    out = torch.zeros(T, dtype=torch.bool, device="cuda")
+    out[::3] = True
+    labels[out] = V
+    w[V // 2, 1], w[V // 3, 2] = float("inf"), float("nan")
+    got = ce_run(x, w, b, labels)
+    assert not bool(got["dx"][out].any()) and not bool(got["row_loss"][out].any())
+    assert bool(torch.isnan(got["row_loss"][~out]).all()) and bool(torch.isnan(got["dx"][~out][:, 2]).all())
+    labels[:] = -1      # no row counts
+    got = ce_run(x, w, b, labels)
+    assert not any(bool(got[k].any()) for k in got)
