@@ -418,7 +418,8 @@ int lp_orthogonalize(int dtype, int batch, int rows, int cols, const void* g, vo
 /* The update with it, in place:  m <- momentum m + g;  u = nesterov ? g + momentum m : m;  O = orthogonalised u;
  *   w <- (1 - lr weight_decay) w - lr scale O
  * w, g in dtype, momentum_buf fp32, all [batch][rows][cols]; w, g and momentum_buf must not overlap.  `scale` is the caller's
- * (for instance sqrt(max(1, rows / cols))).  Scratch, steps, coeffs, eps as in lp_orthogonalize. */
+ * (for instance sqrt(max(1, rows / cols))).  Scratch, steps, coeffs, eps and the precision of O as in lp_orthogonalize; what is
+ * rounded to dtype once is w. */
 int lp_muon_update(int dtype, int batch, int rows, int cols, void* w, const void* g, float* momentum_buf, float lr,
                    float momentum, int nesterov, float weight_decay, float scale, int steps, const float* coeffs, float eps,
                    void* scratch, size_t scratch_bytes, void* stream);

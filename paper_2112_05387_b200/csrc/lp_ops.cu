@@ -209,7 +209,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.aux = s.a; p.aux_f = q.coeffs[1] * (kScaleB / kScaleA); p.diag = q.coeffs[0] * kScaleB;
     rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, cut_a, st);
     if (rc != LP_OK) return rc;
-    // X <- B X (X B).  An error in X grows by up to a in each later step, so where the result itself is wanted the low part
+    // X <- B X (X B).  An error in X grows by up to a in each later step, so but for lp_step_muon (q.low) the low part
     // is kept while three or more products follow (relative error, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3
     // with the low parts of two steps, 1.1e-3 with all; fp16's step in A and B costs 1e-3; a low part costs a product)
     memset(&p, 0, sizeof(p));
@@ -392,7 +392,8 @@ int lp_muon_update(int dtype, int batch, int rows, int cols, void* w, const void
   memset(&q, 0, sizeof(q));
   q.batch = batch; q.rows = rows; q.cols = cols;
   q.g_bf16 = q.out_bf16 = dtype == LP_BF16;
-  q.split = dtype == LP_F32;
+  // (as exact as lp_orthogonalize: rates and weights are the caller's, and beside small or zero weights the step is all there is)
+  q.split = ortho_two_parts(dtype, rows, cols); q.low = true;
   q.g = g; q.momentum = momentum_buf; q.mu = momentum; q.nesterov = nesterov != 0;
   q.out = w; q.update = true; q.keep = 1.f - lr * weight_decay; q.step = -lr * scale;
   q.steps = steps; q.eps = eps;

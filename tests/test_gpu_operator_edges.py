@@ -1,8 +1,8 @@
 """GPU parity of the operators at the end of a training step where values stand that must not matter (rows that do not count,
-masked classes) and where logits are far from 0."""
+masked classes), where logits are far from 0, and at the precision that include/lp.h states."""
 import pytest
 
-from test_gpu_operators import ce_check, ce_inputs, ce_reference, ce_run
+from test_gpu_operators import EPS32, ce_check, ce_inputs, ce_reference, ce_run, muon_reference, ortho_tol, rel, scratch_of, spectrum
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +91,42 @@ def test_rows_that_do_not_count_beside_infinite_weights(size, dtype):
     labels[:] = -1      # no row counts
     got = ce_run(x, w, b, labels)
     assert not any(bool(got[k].any()) for k in got)
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("kind", ["even", "low rank", "decay"])
+@pytest.mark.parametrize("size", [(1, 24, 90), (1, 48, 2000), (1, 64, 576), (1, 200, 700), (2, 256, 512), (1, 512, 256), (1, 520, 520), (1, 257, 1031)], ids=str)
+def test_the_update_in_bf16_is_as_exact_as_the_orthogonalisation(size, kind, nesterov):
+    """Weights of 0 and a rate of 1: the step is all there is to see.  With y the step before its rounding to bf16, off by d from
+    the formula's r, |rn(y) - r| <= |rn(r) - r| + 2 d (see test_few_singular_values_in_bf16_cost_one_rounding).  Smaller side below
+    64: d is LP_F32's bound; else the result is off by 3e-3 of its norm at most.  Then weights that the step is not small beside:
+    their rounding and the step's error."""
+    import torch
+    import paper_2112_05387_b200 as lp
+    B, rows, cols = size
+    small = min(rows, cols)
+    gen = torch.Generator("cuda").manual_seed(12)
+    if kind == "even":
+        g = torch.randn(*size, generator=gen, device="cuda")
+    else:
+        g = torch.stack([spectrum(kind, rows, cols, seed=i) for i in range(B)])
+    g = g.bfloat16()
+    m0 = 0.1 * g.float() * torch.rand(B, 1, 1, generator=gen, device="cuda")
+    buf, at, nb = scratch_of(lp.lp_orthogonalize_scratch_bytes(lp.LP_BF16, *size))
+    for lr, scale, spread in ((1.0, 1.0, 0.0), (0.5, 1.25, 0.05)):
+        w0 = (spread * torch.randn(*size, generator=gen, device="cuda")).bfloat16()
+        w, m = w0.clone(), m0.clone()
+        lp.lp_muon_update(lp.LP_BF16, *size, w, g, m, lr, 0.9, nesterov, 0.1, scale, 5, None, 1e-7, at, nb)
+        assert lp.lp_scratch_status(at) == lp.LP_OK
+        want, want_m = muon_reference(w0, g, m0, lr, 0.9, nesterov, 0.1, scale)
+        step = float((want - (1 - lr * 0.1) * w0.double()).norm())
+        rounding = float((want.bfloat16().double() - want).norm())
+        # (spectra of a few strong directions: LP_F32's bound of test_spectra_of_gradients)
+        d = (ortho_tol("f32") if kind == "even" else 3 * 3.4445 ** 5 * 2.0 ** -22) if small < 64 else 3e-3
+        off = float((w.double() - want).norm())
+        if spread == 0.0 and small >= 64:
+            assert off <= 3e-3 * step
+        else:
+            assert off <= rounding + 2 * d * step
+        assert rel(m, want_m) < 4 * EPS32
+    del buf
