@@ -59,9 +59,14 @@ struct GemmParams {
   int round_len;                  // kRounds: K blocks per accumulation (0: see launch_gemm)
   int a_mn, b_mn;                 // 1: the operand's row index is the contiguous one
   uint32_t idesc;
-  // 1: the kernel before reads and writes nothing of this one's (and has itself waited for what this one reads, before it let
-  // this one start): the two run side by side, and this one waits for that one's end before its own
-  int wait_late;
+  // Two products side by side that read the same operands and write different results: the first (`publish` given) stores `turn`
+  // there once it has waited for the kernels before it, and before it lets the second start; the second (`wait_late`) acquires that
+  // word, by which it sees all that the first saw, and waits for the first one's end before its own.  (A grid's own wait is all
+  // that orders it behind the grids before, so starting without one needs the word; if it is not there yet, it waits after all.
+  // A call clears the word in a kernel that both follow.)
+  int* publish;
+  const int* wait_late;
+  int turn;
   int* err;
   int* clear;                     // two words (the error word is the first) to clear, or null
   // scale of the accumulator: f * f_dev[b]^f_pow
@@ -430,7 +435,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   __syncthreads();
   if constexpr (kCluster) cluster_sync_all();   // both CTAs' barriers exist before anything signals them from the other side
   tc_fence_after();
-  if (!p.wait_late) pdl_wait();
+  if (!p.wait_late || ld_acquire(p.wait_late) != p.turn) pdl_wait();
+  if (p.wait_late) fence_async_global();   // (what was written before is read through TMA)
+  if (p.publish && blockIdx.x == 0 && threadIdx.x == 0) st_release(p.publish, p.turn);
   if (p.clear && blockIdx.x == 0 && threadIdx.x == 0) p.clear[0] = p.clear[1] = 0;   // (a wait gives up after 0.3 s at the earliest)
   pdl_launch_dependents();
   const uint32_t tmem_base = tail->tmem_base;

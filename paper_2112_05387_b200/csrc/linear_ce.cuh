@@ -27,6 +27,7 @@ struct CeHeader {
   float logit_f;      // scale of x w^T's accumulator
   float dx_f, dw_f;   // scales of the gradients' accumulators
   float grad_f;       // g / count
+  int dl_seen;        // pieces of the rows whose dl the product of dx has seen (see GemmParams)
 };
 
 __device__ __forceinline__ bool ce_counts(int label, int V) { return label >= 0 && label < V; }
@@ -168,6 +169,7 @@ ce_pack_kernel(const void* __restrict__ x, const void* __restrict__ w, const voi
       hdr->err = hdr->done = 0;
       hdr->count = counted;
     }
+    hdr->dl_seen = 0;
     const float gf = counted > 0 ? g / (float)counted : 0.f;
     const float dl = is_bf16 ? 1.f : 1.f / kCeDlScale;
     hdr->logit_f = (1.f / scales[0]) * (1.f / scales[1]);

@@ -501,6 +501,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.labels = labels + r0; p.classes = V;   // (0 * inf of w must not reach a row that does not count)
       const GemmCut kd = gemm_cut(rows, D, V, 1, false, planes, planes);
       p.round_len = s.f32 ? ce_round(kd, V) : 0;
+      p.publish = &s.hdr->dl_seen; p.turn = r0 / s.rows + 1;
       if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, kd, st)) != LP_OK) return rc;
       dx_idle = p.total_tiles * kd.ctas < Dv.sm_count;
     }
@@ -514,7 +515,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.out = dw; p.out_bf16 = is_bf16; p.out_ld = D;
       // (beside dx's product where that leaves SMs idle: 64 rows x 512 x 1000 30 us and 33 one after the other, fp32 43 and 48;
       // where it has all of them the two share L2 badly, 4096 x 2048 x 32000 1.32 ms and 1.31)
-      p.wait_late = dx_idle;
+      p.wait_late = dx_idle ? &s.hdr->dl_seen : nullptr; p.turn = r0 / s.rows + 1;
       if (s.rows < T) {
         p.acc = s.f32 ? (float*)dw : s.acc;
         p.acc_first = r0 == 0;

@@ -279,6 +279,18 @@ __host__ __device__ __forceinline__ uint32_t swizzle_code_for_row_bytes(int row_
   return row_bytes == 128 ? 2u : (row_bytes == 64 ? 4u : 6u);
 }
 
+// A word of global memory that hands what this thread has seen on to a thread that reads it, in whichever grid.
+__device__ __forceinline__ void st_release(int* p, int v) {
+  asm volatile("st.release.gpu.global.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+__device__ __forceinline__ int ld_acquire(const int* p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+// Orders what this thread has seen of global memory before its copies through the asynchronous proxy.
+__device__ __forceinline__ void fence_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+
 // ---- CTA pairs (cluster of two, cta_group::2) ----------------------------------------------
 __device__ __forceinline__ uint32_t cluster_ctarank() {
   uint32_t r;

@@ -130,3 +130,53 @@ def test_the_update_in_bf16_is_as_exact_as_the_orthogonalisation(size, kind, nes
             assert off <= rounding + 2 * d * step
         assert rel(m, want_m) < 4 * EPS32
     del buf
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(64, 512, 1000), (300, 64, 2000)], ids=str)
+def test_gradients_side_by_side_see_their_own_call(size, dtype):
+    """Both gradients' products of a small loss run beside one another.  Two sets of inputs in turn through one scratch, called
+    and replayed, with other work on a second stream: every result has the bits of its set taken alone."""
+    import torch
+    import paper_2112_05387_b200 as lp
+    T, D, V = size
+    code = lp.LP_F32 if dtype == "f32" else lp.LP_BF16
+    sets = [ce_inputs(T, D, V, dtype, seed=s, ignored=0.1) for s in (0, 1)]
+    alone = [ce_run(*s) for s in sets]
+    buf, at, n = scratch_of(lp.lp_linear_cross_entropy_scratch_bytes(code, T, D, V, True))
+    outs = [[{k: torch.zeros_like(v) for k, v in alone[0].items()} for _ in range(20)] for _ in range(2)]
+    st, beside = torch.cuda.Stream(), torch.cuda.Stream()
+    a = torch.randn(1024, 1024, device="cuda")
+
+    def calls():
+        for i in range(20):
+            for s in (0, 1):
+                o = outs[s][i]
+                lp.lp_linear_cross_entropy(code, T, D, V, *sets[s], 1.0, o["loss"], o["row_loss"], o["dx"], o["dw"], o["dbias"], at, n, st.cuda_stream)
+
+    def check():
+        torch.cuda.synchronize()
+        assert lp.lp_scratch_status(at, st.cuda_stream) == lp.LP_OK
+        for s in (0, 1):
+            for o in outs[s]:
+                for k in o:
+                    assert torch.equal(o[k], alone[s][k]), k
+                    o[k].zero_()
+        torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=st):
+        calls()
+    for _ in range(4):
+        with torch.cuda.stream(beside):
+            for _ in range(20):
+                a = a @ a * 1e-3
+        calls()
+        check()
+        with torch.cuda.stream(beside):
+            for _ in range(20):
+                a = a @ a * 1e-3
+        with torch.cuda.stream(st):
+            graph.replay()
+        check()
+    del buf
