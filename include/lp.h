@@ -208,9 +208,10 @@ int lp_step(lp_handle* h, float lr, float momentum, float weight_decay, float ka
  * whose gradients are fresh, as a matrix [C_out][R S C_in],
  *     m <- momentum m + g;  u = nesterov ? g + momentum m : m;  O = orthogonalised u (lp_orthogonalize, five steps, 1e-7);
  *     W <- (1 - lr_conv weight_decay) W - lr_conv sqrt(max(1, rows / cols)) O,
- * and the other parameters and the multipliers as in lp_step (rate lr).  The momentum is the one that lp_step keeps.  In LP_BF16
- * O is off by up to 1e-2 of its norm (iterates in fp16), in LP_F32 by some 1e-6.  scratch: lp_step_muon_scratch_bytes() bytes,
- * 256-byte aligned, the call's own while it runs.  LP_ERR_ORDER if no module's gradients are fresh. */
+ * and the other parameters and the multipliers as in lp_step (rate lr).  The momentum is the one that lp_step keeps (and,
+ * as there, is left alone where `momentum` is 0).  O is as exact as that of lp_orthogonalize in the handle's dtype; the weights are
+ * fp32.  scratch: lp_step_muon_scratch_bytes() bytes, 256-byte aligned, the call's own while it runs; a bounded wait that ran out
+ * shows in lp_last_device_status.  LP_ERR_ORDER if no module's gradients are fresh. */
 size_t lp_step_muon_scratch_bytes(lp_handle* h);
 int lp_step_muon(lp_handle* h, float lr_conv, float lr, float momentum, int nesterov, float weight_decay, float kappa_step,
                  void* const* lambdas_inout, void* scratch, size_t scratch_bytes, void* stream);

@@ -2970,20 +2970,20 @@ static void muon_groups(const Plan& P, std::vector<MuonGroup>* groups, std::vect
 }
 // The groups of a module in turn on its stream and on those of its weight gradients (their chains of small products do not fill
 // the machine: ResNet-50 1.27 ms a step on one stream a module, 1.21 on these); each stream has a part of the scratch.
-static std::vector<size_t> muon_lanes(const Plan& P, const std::vector<MuonGroup>& groups, bool split) {
+static std::vector<size_t> muon_lanes(const Plan& P, const std::vector<MuonGroup>& groups, int dtype) {
   std::vector<size_t> bytes(1 + P.side.size(), 0);
   for (size_t i = 0; i < groups.size(); ++i) {
     const MuonGroup& g = groups[i];
     size_t& b = bytes[i % bytes.size()];
-    b = std::max(b, ortho_scratch_bytes((int)g.off.size(), g.rows, g.cols, split));
+    b = std::max(b, ortho_scratch_bytes((int)g.off.size(), g.rows, g.cols, ortho_two_parts(dtype, g.rows, g.cols)));
   }
   return bytes;
 }
-static size_t muon_module_scratch(const Plan& P, bool split) {
+static size_t muon_module_scratch(const Plan& P, int dtype) {
   std::vector<MuonGroup> groups;
   muon_groups(P, &groups, nullptr);
   size_t total = 0;
-  for (size_t b : muon_lanes(P, groups, split)) total += b;
+  for (size_t b : muon_lanes(P, groups, dtype)) total += b;
   return total;
 }
 
@@ -2991,7 +2991,7 @@ size_t lp_step_muon_scratch_bytes(lp_handle* h) {
   if (!h) return 0;
   try {
     size_t total = 0;
-    for (const Plan& P : h->modules) total += muon_module_scratch(P, h->dtype == LP_F32);
+    for (const Plan& P : h->modules) total += muon_module_scratch(P, h->dtype);
     return total;
   } catch (...) {   // (host memory)
     return 0;
@@ -3007,7 +3007,7 @@ static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momen
   std::vector<MuonGroup> groups;
   std::vector<SgdSpans> spans;
   muon_groups(P, &groups, &spans);
-  const std::vector<size_t> bytes = muon_lanes(P, groups, h->dtype == LP_F32);
+  const std::vector<size_t> bytes = muon_lanes(P, groups, h->dtype);
   const size_t lanes = bytes.size();
   apart = apart && lanes > 1 && groups.size() > 1 && can_fork(st, P.side);
   if (apart) LP_CUDA_OK(cudaEventRecord(P.side_ev[0], st));
@@ -3025,7 +3025,7 @@ static int muon_module(lp_handle* h, int k, float lr_conv, float lr, float momen
     OrthoProblem q;
     memset(&q, 0, sizeof(q));
     q.batch = (int)g.off.size(); q.rows = g.rows; q.cols = g.cols;
-    q.split = h->dtype == LP_F32;
+    q.split = ortho_two_parts(h->dtype, g.rows, g.cols);
     q.g = P.ps.g; q.off = g.off.data();
     q.momentum = momentum != 0.f ? P.ps.m : nullptr; q.mu = momentum; q.nesterov = nesterov;
     q.steps = 5; q.eps = 1e-7f;
@@ -3070,7 +3070,7 @@ int lp_step_muon(lp_handle* h, float lr_conv, float lr, float momentum, int nest
   if (!need || scratch_bytes < need) return LP_ERR_WORKSPACE;
   size_t sizes[LP_MAX_MODULES];
   try {
-    for (size_t k = 0; k < h->modules.size(); ++k) sizes[k] = muon_module_scratch(h->modules[k], h->dtype == LP_F32);
+    for (size_t k = 0; k < h->modules.size(); ++k) sizes[k] = muon_module_scratch(h->modules[k], h->dtype);
   } catch (...) {
     return LP_ERR_WORKSPACE;
   }

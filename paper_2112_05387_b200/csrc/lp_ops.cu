@@ -161,7 +161,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     return ortho_run_small(q, src, small_shape, clear_err, st);
   }
   // (a bf16 gradient is exact in one plane)
-  int x_planes = (q.split || (q.low && !(q.g_bf16 && !q.momentum))) ? 2 : 1;
+  int x_planes = q.split || !q.g_bf16 || q.momentum ? 2 : 1;
   bool flat = B == 1 || src.elems % 8 == 0 || q.off;   // every matrix starts on a group of 8 elements
   for (int b = 0; q.off && b < B; ++b) flat = flat && q.off[b] % 8 == 0;
   const bool vec = flat && q.cols % 8 == 0;
@@ -209,9 +209,9 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
     p.aux = s.a; p.aux_f = q.coeffs[1] * (kScaleB / kScaleA); p.diag = q.coeffs[0] * kScaleB;
     rc = launch_gemm<tc::EPI_H16>(p, small, m_a, false, m_a, false, false, cut_a, st);
     if (rc != LP_OK) return rc;
-    // X <- B X (X B).  An error in X grows by up to a in each later step, so but for lp_step_muon (q.low) the low part
-    // is kept while three or more products follow (relative error, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3
-    // with the low parts of two steps, 1.1e-3 with all; fp16's step in A and B costs 1e-3; a low part costs a product)
+    // X <- B X (X B).  An error in X grows by up to a in each later step, so the low part is kept
+    // while three or more products follow (relative error, 256 x 2304 of a decaying spectrum: 5.6e-3 without, 1.5e-3 with the
+    // low parts of two steps, 1.1e-3 with all; fp16's step in A and B costs 1e-3; a low part costs a product)
     memset(&p, 0, sizeof(p));
     p.M = q.rows; p.N = q.cols; p.batch = B; p.err = s.err;
     p.a_planes = tall ? x_planes : planes;
@@ -230,7 +230,7 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
       }
       rc = launch_gemm<tc::EPI_OUT>(p, small, ma, false, mb, !tall, false, cut_x, st);
     } else {
-      x_planes = (q.split || (q.low && i + 3 < q.steps)) ? 2 : 1;
+      x_planes = q.split || i + 3 < q.steps ? 2 : 1;
       cur ^= 1;
       p.h_out = s.x[cur]; p.h_ld = s.ld; p.h_batch = x_mat; p.h_plane = x_planes == 2 ? x_plane : 0;
       rc = launch_gemm<tc::EPI_H16>(p, small, ma, false, mb, !tall, false, cut_x, st);
@@ -244,6 +244,13 @@ int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* 
 
 static_assert(kOrthoMaxOffsets == tc::kGemmMaxOffsets, "one table");
 const float kOrthoCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
+
+// Both parts of everything, for a result in bf16 too where there are few singular values: the roundings of A's and B's diagonals to
+// fp16 then move all of them alike, and where the values lie close together the last steps enlarge that up to 20 times (4 and 24 to
+// 56 of them: errors of 2.5e-3 to 4e-3 of the norm with bf16's own 1.7e-3; from 64 on 1.8e-3 to 2.8e-3, matrices of equal singular
+// values up to 4.3e-3, identities up to 1.02e-2, at 392 rows).  It costs little where latency is what counts (16 x 144 18.0 us and 18.9; 18 x 64 x 576
+// would be 39 and 48).
+bool ortho_two_parts(int dtype, int rows, int cols) { return dtype == LP_F32 || std::min(rows, cols) < 64; }
 
 static int check_ortho(int dtype, int batch, int rows, int cols, int steps, float eps) {
   if (dtype != LP_F32 && dtype != LP_BF16) return LP_ERR_UNSUPPORTED;
@@ -352,12 +359,6 @@ using namespace lp;
 
 extern "C" {
 
-// Both parts of everything, for a result in bf16 too where there are few singular values: the roundings of A's and B's diagonals to
-// fp16 then move all of them alike, and where the values lie close together the last steps enlarge that up to 20 times (4 and 24 to
-// 56 of them: errors of 2.5e-3 to 4e-3 of the norm with bf16's own 1.7e-3; from 64 on 1.8e-3 to 2.3e-3, 400 x 8192 2.9e-3).  It
-// costs little where latency is what counts (16 x 144 18.0 us and 18.9; 18 x 64 x 576 would be 39 and 48).
-static bool ortho_two_parts(int dtype, int rows, int cols) { return dtype == LP_F32 || std::min(rows, cols) < 64; }
-
 size_t lp_orthogonalize_scratch_bytes(int dtype, int batch, int rows, int cols) {
   if (check_ortho(dtype, batch, rows, cols, 1, 1.f) != LP_OK) return 0;
   return ortho_scratch_bytes(batch, rows, cols, ortho_two_parts(dtype, rows, cols));
@@ -375,7 +376,7 @@ int lp_orthogonalize(int dtype, int batch, int rows, int cols, const void* g, vo
   q.batch = batch; q.rows = rows; q.cols = cols;
   q.g_bf16 = q.out_bf16 = dtype == LP_BF16;
   q.split = ortho_two_parts(dtype, rows, cols);
-  q.g = g; q.out = out; q.steps = steps; q.eps = eps; q.low = true;
+  q.g = g; q.out = out; q.steps = steps; q.eps = eps;
   memcpy(q.coeffs, coeffs ? coeffs : kOrthoCoeffs, sizeof(q.coeffs));
   return ortho_run(q, scratch, (cudaStream_t)stream, nullptr);
 }
@@ -393,7 +394,7 @@ int lp_muon_update(int dtype, int batch, int rows, int cols, void* w, const void
   q.batch = batch; q.rows = rows; q.cols = cols;
   q.g_bf16 = q.out_bf16 = dtype == LP_BF16;
   // (as exact as lp_orthogonalize: rates and weights are the caller's, and beside small or zero weights the step is all there is)
-  q.split = ortho_two_parts(dtype, rows, cols); q.low = true;
+  q.split = ortho_two_parts(dtype, rows, cols);
   q.g = g; q.momentum = momentum_buf; q.mu = momentum; q.nesterov = nesterov != 0;
   q.out = w; q.update = true; q.keep = 1.f - lr * weight_decay; q.step = -lr * scale;
   q.steps = steps; q.eps = eps;

@@ -8,9 +8,7 @@ namespace lp {
 struct OrthoProblem {
   int batch, rows, cols;
   bool g_bf16;            // type of g
-  bool split;             // fp32 results: operands as high and low parts
-  bool low;               // else: the low parts of the first iterates are kept.  lp_step_muon does without: O is then off by up to 1e-2
-                          // of its norm, as lp.h says there (2 x 4096 x 4096 2.4 ms and 3.0)
+  bool split;             // operands as high and low parts in all steps (ortho_two_parts); else X in the first ones
   const void* g;
   const long long* off;   // element offset of each matrix from g, momentum and out (host; at most kOrthoMaxOffsets matrices then),
                           // or null: one after another
@@ -29,6 +27,7 @@ struct OrthoProblem {
 
 constexpr int kOrthoMaxOffsets = 64;
 extern const float kOrthoCoeffs[3];
+bool ortho_two_parts(int dtype, int rows, int cols);
 size_t ortho_scratch_bytes(int batch, int rows, int cols, bool split);
 // Enqueues the operator; `launches` (nullable) counts its kernels.
 int ortho_run(const OrthoProblem& q, void* scratch, cudaStream_t st, long long* launches);

@@ -2,7 +2,8 @@
 masked classes), where logits are far from 0, and at the precision that include/lp.h states."""
 import pytest
 
-from test_gpu_operators import EPS32, ce_check, ce_inputs, ce_reference, ce_run, muon_reference, ortho_tol, rel, scratch_of, spectrum
+from test_gpu_operators import EPS32, ce_check, ce_inputs, ce_reference, ce_run, muon_reference, ortho_reference, ortho_tol, \
+    rel, scratch_of, spectrum
 
 pytestmark = pytest.mark.gpu
 
@@ -179,4 +180,46 @@ def test_gradients_side_by_side_see_their_own_call(size, dtype):
         with torch.cuda.stream(st):
             graph.replay()
         check()
+    del buf
+
+
+@pytest.mark.parametrize("name", ["small_preact_bf16", "wrn28_10", "tiny"])
+def test_the_step_is_as_exact_as_stated(name):
+    """include/lp.h: O of lp_step_muon is as exact as lp_orthogonalize's, 4e-3 of its norm in LP_BF16 and 5e-5 in LP_F32.  No decay, a rate of 1: the weights
+    (fp32) move by the step alone, and are rounded by half a step of fp32 once."""
+    import numpy as np
+    import torch
+    import paper_2112_05387_b200 as lp
+    from conftest import small_cfg
+    from harness import GpuRun
+    from workloads import scaled
+    cfg = {"tiny": lambda: scaled("tiny"), "small_preact_bf16": lambda: small_cfg("preact", dtype="bf16", stage_channels=(16, 32)),
+           "wrn28_10": lambda: scaled("wrn28_10", N=2)}[name]()
+    run = GpuRun(cfg)
+    K, f32 = run.net.K, cfg["dtype"] == "f32"
+    buf, at, nb = scratch_of(lp.lp_step_muon_scratch_bytes(run.h))
+    gen = torch.Generator("cuda").manual_seed(14)
+    dt = torch.float32 if f32 else torch.bfloat16
+    x = [torch.randn(*run.net.boundary[k], generator=gen, device="cuda").to(dt) for k in range(K)]
+    labels = torch.randint(0, cfg["num_classes"], (cfg["N"],), generator=gen, device="cuda", dtype=torch.int32)
+    loss = torch.zeros(K, 2, device="cuda")
+    lp.lp_modules_fwd_bwd_all(run.h, x, labels, None, 0.7, loss, None)
+    before = [lp.lp_get_params(run.h, k).astype(np.float64) for k in range(K)]
+    grads = [lp.lp_get_grads(run.h, k).astype(np.float64) for k in range(K)]
+    lp.lp_step_muon(run.h, 1.0, 0.0, 0.0, False, 0.0, 0.0, None, at, nb)
+    assert lp.lp_last_device_status(run.h) == 0
+    worst = 0.0
+    for k in range(K):
+        after, off = lp.lp_get_params(run.h, k).astype(np.float64), 0
+        for pname, kind, shape in run.net.param_layout(k):
+            n = int(np.prod(shape))
+            if kind == "conv_w":
+                g = torch.from_numpy(grads[k][off:off + n].reshape(1, shape[0], n // shape[0]).copy()).cuda()
+                o = ortho_reference(g)[0].cpu().numpy().reshape(-1) * max(1.0, shape[0] * shape[0] / n) ** 0.5
+                p0 = before[k][off:off + n]
+                error = np.linalg.norm(after[off:off + n] - (p0 - o))
+                rounding = EPS32 * (np.linalg.norm(p0) + np.linalg.norm(o))
+                worst = max(worst, (error - rounding) / np.linalg.norm(o))
+            off += n
+    assert worst < (5e-5 if f32 else 4e-3)
     del buf
