@@ -409,9 +409,12 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
  * coeffs: host float[3] = { a, b, c }, or NULL for { 3.4445, -4.7750, 2.0315 }, which take the singular values near 1 in five
  * steps.  out may be g.  batch <= 65535, sides up to 2^24, the smaller one up to 2^17; 1 <= steps <= 32, 1e-30 <= eps <= 1e30; coefficients under which a singular value of X passes 15, or one of
  * b X X^T + c (X X^T)^2 passes 60, overflow.  A matrix that holds NaN or an infinity becomes NaN, no other matrix does.
- * LP_BF16: iterates are kept in fp16 (11 significant bits, the first ones in two parts), the result is off by 2e-3
- * (up to 3e-3 where all singular values are alike) of its norm, of which bf16's own rounding is 1.7e-3.  LP_F32, and LP_BF16 where
- * the smaller side is below 64: every operand is kept in two parts. */
+ * LP_BF16: iterates are kept in fp16 (11 significant bits, the first ones in two parts); the result is off by 2e-3 of its norm, of
+ * which bf16's own rounding is 1.7e-3, for most matrices, by up to 4e-3 for those of a few directions alone, by up to 5e-3 where
+ * all singular values are alike and 1.1e-2 for multiples of the identity, where one rounding moves all values together.  LP_F32, and
+ * LP_BF16 where the smaller side is below 64: every operand is kept in two parts; some 1e-6 of the norm, up to 5e-5 for a few
+ * directions alone, before the rounding to bf16.  Entries are kept to some 1e-9 at best: of a matrix whose norm is many
+ * orders of magnitude below eps nothing is left. */
 size_t lp_orthogonalize_scratch_bytes(int dtype, int batch, int rows, int cols);
 int lp_orthogonalize(int dtype, int batch, int rows, int cols, const void* g, void* out, int steps, const float* coeffs,
                      float eps, void* scratch, size_t scratch_bytes, void* stream);
