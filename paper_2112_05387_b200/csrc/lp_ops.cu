@@ -272,6 +272,7 @@ static const int kCeAmaxParts = 592;
 // where K is shared and short, 2e-7 to 4e-7, at no cost that shows.
 static int ce_round(const GemmCut& cut, long long K) { return cut.kind == tc::GEMM_KSPLIT && K <= 4096 ? 2 : 4; }
 static const int kCeLongRound = 64;         // and of bf16 logits: each of its 256 steps is cut off, 4096 features 1e-6 of the loss
+static const int kCeFewRows = 4;            // the loss alone of so many is one pass over w
 static const int kCeFewBlocks = 592;        // four an SM
 static const size_t kCeFewSmem = 96 * 1024;
 
@@ -301,7 +302,9 @@ static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) 
   s.target = c.take<float>(T);
   s.lse = c.take<float>(T);
   s.row_loss = c.take<float>(T);
-  s.stats = c.take<float2>((size_t)std::max(4 * ((V + 127) / 128), kCeFewBlocks) * s.rows);
+  // (parts of 32 columns at least; a part a block where a few rows' loss is one pass over w)
+  const int tiles32 = 4 * ((V + 127) / 128);
+  s.stats = c.take<float2>((size_t)(!grads && T <= kCeFewRows ? std::max(tiles32, kCeFewBlocks) : tiles32) * s.rows);
   const bool pack_x = s.pack_w || grads;
   s.x = pack_x ? c.take<__half>((size_t)planes * T * s.ld_d) : nullptr;
   s.w = s.pack_w ? c.take<__half>((size_t)planes * V * s.ld_d) : nullptr;
@@ -312,7 +315,6 @@ static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) 
 }
 
 // Loss alone of a few rows.
-static const int kCeFewRows = 4;
 template <typename T, int kRows>
 static int start_few(const CeScratch& s, int rows, int D, int V, const T* x, const T* w, const T* bias, const int32_t* labels, int blocks,
                      cudaStream_t st) {

@@ -88,6 +88,19 @@ def test_scratch_is_bounded_where_the_logits_are_not():
     assert lp.lp_linear_cross_entropy_scratch_bytes(lp.LP_BF16, T, D, V, False) < (520 << 20)
 
 
+def test_scratch_of_few_classes_goes_by_the_classes():
+    """Beside the packed features and two planes of exponentials: 8 bytes a row and 32 classes, three floats a row, the largest
+    magnitudes and the column sums of 64 rows each, every region on 256 bytes."""
+    for dtype, planes in ((lp.LP_F32, 2), (lp.LP_BF16, 1)):
+        for T, D, V in ((262144, 64, 10), (100000, 8, 1000)):
+            ld_v, ld_d, parts = (V + 31) // 32 * 32, (D + 7) // 8 * 8, 4 * ((V + 127) // 128)
+            operands = 2 * planes * (T + V) * ld_d
+            alone = operands + T * (8 * parts + 12) + (1 << 16)
+            assert 0 < lp.lp_linear_cross_entropy_scratch_bytes(dtype, T, D, V, False) <= alone
+            with_grads = alone + 2 * planes * T * ld_v + (T // 64 + 4) * V * 4 + V * D * 4
+            assert 0 < lp.lp_linear_cross_entropy_scratch_bytes(dtype, T, D, V, True) <= with_grads
+
+
 def test_step_and_status_need_a_handle_and_a_scratch():
     lib = lp.library()
     assert lib.lp_step_muon_scratch_bytes(None) == 0
