@@ -386,19 +386,23 @@ int lp_conv2d_fwd_noalloc(int N, int H, int W, int Cin, int Cout, int R, int str
  * the same bits.
  */
 
-/* Softmax cross entropy of a linear layer over V classes, without storing the logits:
+/* Softmax cross entropy of a linear layer over V classes.  The logits are not stored; the gradients keep 16-bit exponentials (two
+ * parts in LP_F32) of a piece of the rows:
  *   l = x w^T + bias;  row_loss[t] = log sum_v exp l[t][v] - l[t][labels[t]];  loss = mean of row_loss over the counted rows
  * A row counts if its label is a class, 0 <= labels[t] < V; any other label leaves the row out: its row_loss and its row of dx
- * are 0 and nothing of x[t] (which may hold anything, NaN included) reaches dw or dbias.
+ * are 0 and nothing of x[t] (which may hold anything, NaN included) reaches another row, dw or dbias.
  *   T from 1 to 2^28, V to 2^24, D to 2^20; x [T][D], w [V][D], bias [V] or NULL, labels int32 [T]
  *   (entries of bias may be -inf: that class then has probability 0, and its row of w may hold anything with which x w^T is finite)
  *   loss_out: float[2] = { loss (0 if no row counts), number of counted rows }; row_loss: float[T] or NULL
  *   dx [T][D], dw [V][D], dbias [V]: grad_scale times the gradient of loss, any of them NULL; overwritten.  All NULL: the loss
  *     alone.
  * In LP_F32 products are taken from 22 bits of each operand, relative to the largest magnitude in the rows of x that count and in
- * the rows of w whose class is not masked by a bias of -inf.  A row whose
- * logits are all -inf has a loss and gradients of NaN, as the formula does.  The inputs are not changed; outputs must not
- * overlap inputs.  The gradients take the rows in pieces whose exponentials fit 512 MB (256 rows at least). */
+ * the rows of w whose class is not masked by a bias of -inf.  A row whose logits are all -inf has a loss and gradients of NaN, as
+ * the formula does.  The inputs are not changed; outputs must not overlap inputs.
+ * Scratch: a piece is as many rows as have 512 MB of exponentials, 256 at least and 2^18 at most, or in LP_BF16 all rows where
+ * their exponentials take no more than 4 V D bytes, the fp32 sums of dw that several pieces need.  Beside it stand x (and w, in
+ * LP_F32 or where D is no multiple of 8) in 16-bit parts, up to 8 bytes for each row of a piece and 32 classes, and, for
+ * gradients, 4 bytes for each class and 64 rows. */
 size_t lp_linear_cross_entropy_scratch_bytes(int dtype, int T, int D, int V, int grads);
 int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const void* w, const void* bias,
                             const int32_t* labels, float grad_scale, float* loss_out, float* row_loss, void* dx, void* dw,
@@ -407,8 +411,9 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
 /* Orthogonalisation by Newton-Schulz products, of `batch` matrices G [rows][cols] one after another in memory:
  *   X = G / max(|G|_F, eps);  `steps` times  X <- a X + b (X X^T) X + c (X X^T)^2 X;  out = X
  * coeffs: host float[3] = { a, b, c }, or NULL for { 3.4445, -4.7750, 2.0315 }, which take the singular values near 1 in five
- * steps.  out may be g.  batch <= 65535, sides up to 2^24, the smaller one up to 2^17; 1 <= steps <= 32, 1e-30 <= eps <= 1e30; coefficients under which a singular value of X passes 15, or one of
- * b X X^T + c (X X^T)^2 passes 60, overflow.  A matrix that holds NaN or an infinity becomes NaN, no other matrix does.
+ * steps.  out may be g.  batch <= 65535, sides up to 2^24, the smaller one up to 2^17; 1 <= steps <= 32, 1e-30 <= eps <= 1e30;
+ * coefficients under which a singular value of X passes 15, or one of b X X^T + c (X X^T)^2 passes 60, overflow.  A matrix that
+ * holds NaN or an infinity becomes NaN, no other matrix does.
  * LP_BF16: iterates are kept in fp16 (11 significant bits, the first ones in two parts); the result is off by 2e-3 of its norm, of
  * which bf16's own rounding is 1.7e-3, for most matrices, by up to 4e-3 for those of a few directions alone, by up to 5e-3 where
  * all singular values are alike and 1.1e-2 for multiples of the identity, where one rounding moves all values together.  LP_F32, and

@@ -1,5 +1,5 @@
 // What every translation unit of the library needs on the host: the record of a device (SM count, tensor-map encoder, kernel
-// attributes set so far), error and size helpers, launches on clusters of two CTAs.
+// attributes set so far), error and size helpers, launches on clusters.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -39,7 +39,7 @@ struct Device {
   int max_pairs = 0;   // CTA pairs of conv_tc2_kernel that can be resident at once (0: not usable)
   int gemm_pairs = 0;  // the same for gemm_tc_kernel
   int small_clusters[9] = {0}; // clusters of 1, 2, 4, 8 CTAs of ortho_small_kernel
-  int gemm_clusters[9] = {0};  // and its clusters of 2 to 8 CTAs that share K
+  int gemm_clusters[9] = {0};  // and its clusters of kKShares CTAs (gemm_launch.h) that share K
   int init() {
     if (ready) return LP_OK;
     int dev = 0;

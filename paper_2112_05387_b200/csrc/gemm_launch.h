@@ -57,6 +57,8 @@ static int max_clusters(int ctas, void (*kernel)(KArgs...), int threads, size_t 
   if (cudaOccupancyMaxActiveClusters(&n, kernel, &q) != cudaSuccess) { cudaGetLastError(); n = 0; }
   return n;
 }
+// Sizes of the clusters that share K.
+static const int kKShares[] = {2, 3, 4, 8};
 // Kernel attributes, and how many CTA pairs the device holds at once (the grid is persistent: never more than that).
 static int gemm_init_dev() {
   int rc = init_cur_dev();
@@ -73,7 +75,7 @@ static int gemm_init_dev() {
       (rc = gemm_set_attributes<EPI_OUT, GEMM_LONG>()) != LP_OK)
     return rc;
   D.gemm_pairs = max_clusters(2, gemm_tc_kernel<EPI_OUT, GEMM_PAIR, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
-  for (int c = 2; c <= 8; ++c)
+  for (int c : kKShares)
     D.gemm_clusters[c] = max_clusters(c, gemm_tc_kernel<EPI_OUT, GEMM_KSPLIT, GEMM_ONE>, kGemmThreads, kGemmSmem, D.sm_count);
   D.gemm_attr = true;
   return LP_OK;
@@ -115,8 +117,8 @@ static GemmCut gemm_cut(long long M, long long N, long long K, int batch, bool s
       if (t_half < time) { best = GemmCut{tc::GEMM_HALF, 2}; time = t_half; }
     }
   }
-  for (int c = 2; c <= 8 && c <= kb; c += c < 4 ? 1 : 4) {
-    if (D.gemm_clusters[c] < 1) continue;
+  for (int c : kKShares) {
+    if (c > kb || D.gemm_clusters[c] < 1) continue;
     const long long t = (((kb + c - 1) / c + 2) * c_single + (products == 3 ? 2500 : 4500) + (c == 8 ? 3000 : 0)) * waves(count(128, 128), D.gemm_clusters[c]);
     if (t < time) { best = GemmCut{tc::GEMM_KSPLIT, c}; time = t; }
   }

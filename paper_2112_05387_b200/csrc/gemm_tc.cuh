@@ -446,7 +446,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int steps = kKSplit ? p.kblocks * (int)(crank + 1) / ctas - k_first : p.kblocks;
   constexpr bool kRounds = kMode == GEMM_SPLIT || kMode == GEMM_LONG;
   const int round_len = kRounds ? p.round_len : steps;
-  constexpr uint32_t kTiles = kMode == GEMM_SPLIT ? 4 : kMode == GEMM_LOW ? 3 : 2, kStages = kHalf ? 4 : 12 / kTiles, kStageBytes = kHalf ? 2 * (kGemmTileBytes + kTileBytesB) : kTiles * kGemmTileBytes;
+  constexpr uint32_t kTiles = kMode == GEMM_SPLIT ? 4 : kMode == GEMM_LOW ? 3 : 2;
+  constexpr uint32_t kStages = kHalf ? 4 : 12 / kTiles;
+  constexpr uint32_t kStageBytes = kHalf ? 2 * (kGemmTileBytes + kTileBytesB) : kTiles * kGemmTileBytes;
   static_assert(kStages <= kGemmStages && kStages * kStageBytes <= kGemmRingBytes, "the ring");
   // (GEMM_LOW: which operand has two parts is known at run time)
   const int a_planes = kMode == GEMM_SPLIT ? 2 : (kMode == GEMM_LOW ? p.a_planes : 1);
@@ -519,7 +521,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             tc_fence_after();
             const uint32_t at = base + s * kStageBytes;
             auto product = [&](int x, int y, uint32_t more) {   // tiles x (of A) and y (of B) of the stage
-              const uint64_t ad = smem_desc(da, at + x * kGemmTileBytes), bd = smem_desc(db, at + (kHalf ? 2 * kGemmTileBytes + (y - 2) * kTileBytesB : y * kGemmTileBytes));
+              const uint32_t of_b = kHalf ? 2 * kGemmTileBytes + (y - 2) * kTileBytesB : y * kGemmTileBytes;
+              const uint64_t ad = smem_desc(da, at + x * kGemmTileBytes), bd = smem_desc(db, at + of_b);
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 if constexpr (kPair) mma2_bf16(d, ad + (uint64_t)(j * ka), bd + (uint64_t)(j * kb16), p.idesc, j ? 1u : more);

@@ -476,7 +476,8 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     p.round_len = s.f32 ? ce_round(cut, D) : kCeLongRound;
     if (!s.x && r0 == 0) p.clear = &s.hdr->err;   // (no kernel before that could have)
     if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, cut, st)) != LP_OK) return rc;
-    // few rows and parts: one block does the rest of the loss
+    // few rows and parts: one block does the rest of the loss (us with it and without: 16 x 512 x 4000 in fp32, the loss alone, 23.0 and
+    // 24.1; 64 x 512 x 1000 with gradients 39.4 and 38.9; in bf16 the loss alone of 256 rows or of 500 parts 22 or 18 and 15)
     const bool finished = rows == T && rows <= 64 && parts <= 128;
     if (finished)
       LP_CUDA_OK(launch_pdl(ce_finish_kernel, dim3(1), dim3(1024), 0, st, (const float2*)s.stats, (long long)s.rows, parts, rows, V, labels,
