@@ -397,8 +397,8 @@ int lp_conv2d_fwd_noalloc(int N, int H, int W, int Cin, int Cout, int R, int str
  *   dx [T][D], dw [V][D], dbias [V]: grad_scale times the gradient of loss, any of them NULL; overwritten.  All NULL: the loss
  *     alone.
  * In LP_F32 products are taken from 22 bits of each operand, relative to the largest magnitude in the rows of x that count and in
- * the rows of w whose class is not masked by a bias of -inf.  A row whose logits are all -inf has a loss and gradients of NaN, as
- * the formula does.  The inputs are not changed; outputs must not overlap inputs.
+ * the rows of w whose class is not masked by a bias of -inf; the sums of dx and dw are off by less than 1e-6 of their norms.  A row
+ * whose logits are all -inf has a loss and gradients of NaN, as the formula does.  The inputs are not changed; outputs must not overlap inputs.
  * Scratch: a piece is as many rows as have 512 MB of exponentials, 256 at least and 2^18 at most, or in LP_BF16 all rows where
  * their exponentials take no more than 4 V D bytes, the fp32 sums of dw that several pieces need.  Beside it stand x (and w, in
  * LP_F32 or where D is no multiple of 8) in 16-bit parts, up to 8 bytes for each row of a piece and 32 classes, and, for

@@ -268,9 +268,10 @@ static int check_ortho(int dtype, int batch, int rows, int cols, int steps, floa
 // one piece.
 static const size_t kCePieceBytes = (size_t)512 << 20;
 static const int kCeAmaxParts = 592;
-// K blocks an accumulation (fp32 problems).  Four: 3e-7 to 9e-7 of a gradient, 1001 x 640 x 20011 339 us (two: 354, one: 371); two
-// where K is shared and short, 2e-7 to 4e-7, at no cost that shows.
-static int ce_round(const GemmCut& cut, long long K) { return cut.kind == tc::GEMM_KSPLIT && K <= 4096 ? 2 : 4; }
+// K blocks an accumulation (fp32 problems): 24 steps of the tensor core, each of which cuts the sum off by 2^-25 of it on average.  Worst
+// gradients of 150 problems, and 1001 x 640 x 20011: one block 4e-7 of the norm and 350 us, two 6e-7 and 327, four 1.5e-6 and 312; plain
+// fp32 products 5e-7.
+static const int kCeRound = 2;
 static const int kCeLongRound = 64;         // and of bf16 logits: each of its 256 steps is cut off, 4096 features 1e-6 of the loss
 static const int kCeFewRows = 4;            // the loss alone of so many is one pass over w
 static const int kCeFewBlocks = 592;        // four an SM
@@ -473,7 +474,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     p.bias = bias; p.bias_bf16 = is_bf16; p.labels = labels + r0;
     p.stats = s.stats; p.stats_ld = s.rows; p.target = s.target + r0;
     p.h_out = s.p; p.h_ld = s.ld_v; p.h_plane = s.f32 ? p_plane : 0;
-    p.round_len = s.f32 ? ce_round(cut, D) : kCeLongRound;
+    p.round_len = s.f32 ? kCeRound : kCeLongRound;
     if (!s.x && r0 == 0) p.clear = &s.hdr->err;   // (no kernel before that could have)
     if ((rc = launch_gemm<tc::EPI_CE>(p, D, m_xk, false, m_wk, false, !s.f32, cut, st)) != LP_OK) return rc;
     // few rows and parts: one block does the rest of the loss (us with it and without: 16 x 512 x 4000 in fp32, the loss alone, 23.0 and
@@ -504,7 +505,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.out = (uint8_t*)dx + (size_t)r0 * D * esize(dtype); p.out_bf16 = is_bf16; p.out_ld = D;
       p.labels = labels + r0; p.classes = V;   // (0 * inf of w must not reach a row that does not count)
       const GemmCut kd = gemm_cut(rows, D, V, 1, false, planes, planes);
-      p.round_len = s.f32 ? ce_round(kd, V) : 0;
+      p.round_len = s.f32 ? kCeRound : 0;
       p.publish = &s.hdr->dl_seen; p.turn = r0 / s.rows + 1;
       if ((rc = launch_gemm<tc::EPI_OUT>(p, V, m_pk, false, m_wm, true, !s.f32, kd, st)) != LP_OK) return rc;
       dx_idle = p.total_tiles * kd.ctas < Dv.sm_count;
@@ -526,7 +527,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
         p.acc_last = r0 + rows == T;
       }
       const GemmCut kd = gemm_cut(V, D, rows, 1, false, planes, planes);
-      p.round_len = s.f32 ? ce_round(kd, rows) : 0;
+      p.round_len = s.f32 ? kCeRound : 0;
       if ((rc = launch_gemm<tc::EPI_OUT>(p, rows, m_pm, true, m_xm, true, !s.f32, kd, st)) != LP_OK) return rc;
     }
   }

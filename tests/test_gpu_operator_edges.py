@@ -263,3 +263,16 @@ def test_the_step_is_as_exact_as_stated(name):
             off += n
     assert worst < (5e-5 if f32 else 4e-3)
     del buf
+
+
+@pytest.mark.parametrize("size", [(1, 699, 16307), (2, 41, 4994), (3, 27, 12087), (3, 1203, 6259), (1, 307, 30), (1, 3553, 274), (4, 731, 300), (16, 1497, 300), (261, 32, 2),
+                                  (1001, 640, 20011), (6140, 468, 3), (6599, 198, 4)], ids=str)
+def test_gradients_in_fp32_are_as_exact_as_stated(size):
+    """Two K blocks an accumulation are 24 steps of the tensor core, each of which cuts the sum off by 2^-25 of it on average: 7.2e-7
+    where a term of the first step is all of it (a row's label in dx, a row in dw).  Operands of 22 bits: 2^-22.  Together less
+    than 1e-6."""
+    T, D, V = size
+    x, w, b, labels = ce_inputs(T, D, V, "f32", seed=15)
+    got, ref = ce_run(x, w, b, labels), ce_reference(x, w, b, labels)
+    for k in ("dx", "dw"):
+        assert rel(got[k], ref[k]) < 1e-6, k
