@@ -694,7 +694,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         // (a half without any class: its exponentials are 0, and `stats` says -inf, so that what they are multiplied by later is
         // 0, too, however low the row's lse is)
         const float ref = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
+        float sums[4] = {0.f, 0.f, 0.f, 0.f};   // (a fourth of the roundings of one chain, next to the largest term, 1)
 #pragma unroll 1
         for (int g = 0; g < groups; ++g) {
           const int col = col0 + g * 32;
@@ -710,10 +710,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             v[j] = exp2f(fmaf(v[j] - ref, kLog2e, kCeExpBits));
-            sum += v[j];
+            sums[j & 3] += v[j];
           }
           if (p.h_out && col < p.N && row0 < p.M) epi_h16(p, 0, row0, lane, col, false, v, scratch);
         }
+        const float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
         if (row < p.M) p.stats[(long long)(col0 / (kKSplit ? 32 : kTileN / 2)) * p.stats_ld + row] = make_float2(top, sum * 6.103515625e-5f);
       } else {
         const bool mirror = p.sym && tm != tn;

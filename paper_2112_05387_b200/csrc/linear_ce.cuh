@@ -272,11 +272,16 @@ __device__ __forceinline__ void ce_join_warp(float& m, float& s) {
   }
 }
 
-// lse and loss of each row from its parts: 8 rows a block (64 bytes of each part), 32 threads a row.  On the last piece of the
+// Loss of a row from its maximum and the sum of exponentials relative to it.  lse stays in these two parts, for the gradients `top` and,
+// in the place of the label's logit, the logarithm: where that logit is the maximum, the loss is the logarithm alone, and a rounding
+// of lse itself (2^-24 of logits that may be large) would be most of a small loss and of its gradients.
+__device__ __forceinline__ float ce_row_loss(float m, float log_sum, float target) { return (m - target) + log_sum; }
+
+// Loss of each row from its parts, and what the gradients need of lse: 8 rows a block (64 bytes of each part), 32 threads a row.  On the last piece of the
 // rows (`loss` given) the block that finishes last takes the mean over the counted rows of all T, in the order of the rows.
 __global__ void __launch_bounds__(kCeThreads)
 ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, int r0, int rows, int T, int V,
-               const int32_t* __restrict__ labels, const float* __restrict__ target, float* __restrict__ lse, float* __restrict__ row_loss,
+               const int32_t* __restrict__ labels, float* __restrict__ target, float* __restrict__ top, float* __restrict__ row_loss,
                CeHeader* __restrict__ hdr, float* __restrict__ loss) {
   pdl_wait();
   pdl_launch_dependents();
@@ -294,9 +299,10 @@ ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, 
   s = ss[warp][lane];
   ce_join_warp(m, s);
   if (lane == 0 && t < rows) {
-    const float l = m + logf(s);
-    lse[r0 + t] = l;
-    row_loss[r0 + t] = ce_counts(labels[r0 + t], V) ? l - target[r0 + t] : 0.f;
+    const float l = logf(s);
+    row_loss[r0 + t] = ce_counts(labels[r0 + t], V) ? ce_row_loss(m, l, target[r0 + t]) : 0.f;
+    top[r0 + t] = m;
+    target[r0 + t] = l;
     __threadfence();
   }
   if (!loss) return;
@@ -326,26 +332,28 @@ ce_rows_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, 
   }
 }
 
-// All of it at once for few rows and parts, in one block: lse and loss of each row, a warp each, the number of counted rows and
+// All of it at once for few rows and parts, in one block: the loss of each row, a warp each, the number of counted rows and
 // the mean.
 __global__ void __launch_bounds__(1024)
 ce_finish_kernel(const float2* __restrict__ stats, long long stats_ld, int parts, int rows, int V, const int32_t* __restrict__ labels,
-                 const float* __restrict__ target, float* __restrict__ lse, float* __restrict__ row_loss, float* __restrict__ loss) {
+                 float* __restrict__ target, float* __restrict__ top, float* __restrict__ row_loss, float* __restrict__ loss) {
   pdl_wait();
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   double total = 0.0;
   int count = 0;
   for (int row = warp; row < rows; row += 32) {
+    // (read ahead of the parts)
+    const bool counts = ce_counts(labels[row], V);
+    const float logit = target[row];
     float m = -INFINITY, s = 0.f;
     ce_join_parts<4>(m, s, stats + row, stats_ld, lane, parts);
     ce_join_warp(m, s);
-    const float l = m + logf(s);
-    const bool counts = ce_counts(labels[row], V);
-    const float x = counts ? l - target[row] : 0.f;
+    const float l = logf(s), x = counts ? ce_row_loss(m, l, logit) : 0.f;
     if (lane == 0) {
-      lse[row] = l;
       row_loss[row] = x;
+      top[row] = m;
+      target[row] = l;
     }
     total += (double)x;
     count += counts;
@@ -450,8 +458,8 @@ constexpr int kCeSlab = 64;
 template <bool kF32>
 __global__ void __launch_bounds__(kCeThreads)
 ce_dl_kernel(__half* __restrict__ p, long long ld, long long plane, int rows, int V, const float2* __restrict__ stats, long long stats_ld,
-             int part_cols, const float* __restrict__ lse, const float* __restrict__ target, const int32_t* __restrict__ labels,
-             float* __restrict__ sums /* [slab][V] or null */, void* __restrict__ dbias /* or null */, const CeHeader* __restrict__ hdr) {
+             int part_cols, const float* __restrict__ top, const float* __restrict__ log_sum, const float* __restrict__ row_loss,
+             const int32_t* __restrict__ labels, float* __restrict__ sums /* [slab][V] or null */, void* __restrict__ dbias /* or null */, const CeHeader* __restrict__ hdr) {
   pdl_wait();
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -464,14 +472,15 @@ ce_dl_kernel(__half* __restrict__ p, long long ld, long long plane, int rows, in
     for (int r0 = blockIdx.y * kCeSlab + warp; r0 < r1; r0 += 8 * kBatch) {
       uint4 hs[kBatch], ls[kF32 ? kBatch : 1];
       int labels_r[kBatch];
-      float lses[kBatch], refs[kBatch];
+      float tops[kBatch], logs[kBatch], refs[kBatch];
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         const int r = min(r0 + 8 * k, r1 - 1);
         hs[k] = *reinterpret_cast<const uint4*>(p + (long long)r * ld + col);
         if constexpr (kF32) ls[k] = *reinterpret_cast<const uint4*>(p + plane + (long long)r * ld + col);
         labels_r[k] = labels[r];
-        lses[k] = lse[r];
+        tops[k] = top[r];
+        logs[k] = log_sum[r];
         refs[k] = ref[r].x;
       }
 #pragma unroll
@@ -481,7 +490,7 @@ ce_dl_kernel(__half* __restrict__ p, long long ld, long long plane, int rows, in
         __half* q = p + (long long)r * ld + col;
         float v[8];
         if (ce_counts(label, V)) {
-          const float f = exp2f(fmaf(refs[k] - lses[k], tc::kLog2e, -tc::kCeExpBits));
+          const float f = exp2f(fmaf((refs[k] - tops[k]) - logs[k], tc::kLog2e, -tc::kCeExpBits));
           const uint32_t u[4] = {hs[k].x, hs[k].y, hs[k].z, hs[k].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) tc::half2_floats(u[i], v[2 * i], v[2 * i + 1]);
@@ -498,7 +507,7 @@ ce_dl_kernel(__half* __restrict__ p, long long ld, long long plane, int rows, in
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] *= f;
           if (label >= col && label < col + 8) {
-            const float d = expm1f(target[r] - lses[k]);   // p - 1 without the cancellation
+            const float d = expm1f(-row_loss[r]);   // p - 1 without the cancellation
 #pragma unroll
             for (int j = 0; j < 8; ++j)
               if (col + j == label) v[j] = d;

@@ -279,7 +279,7 @@ static const size_t kCeFewSmem = 96 * 1024;
 
 struct CeScratch {
   CeHeader* hdr;
-  float *amax, *target, *lse, *row_loss, *sums, *acc;
+  float *amax, *target, *top, *row_loss, *sums, *acc;
   float2* stats;
   __half *p, *x, *w;
   long long ld_v, ld_d;
@@ -301,7 +301,7 @@ static CeScratch ce_carve(Carve& c, int dtype, int T, int D, int V, bool grads) 
   s.hdr = c.take<CeHeader>(1);
   s.amax = c.take<float>(2 * kCeAmaxParts);
   s.target = c.take<float>(T);
-  s.lse = c.take<float>(T);
+  s.top = c.take<float>(T);
   s.row_loss = c.take<float>(T);
   // (parts of 32 columns at least; a part a block where a few rows' loss is one pass over w)
   const int tiles32 = 4 * ((V + 127) / 128);
@@ -333,7 +333,7 @@ static int ce_few_rows(const CeScratch& s, int rows, int D, int V, const T* x, c
                              : start_few<T, 4>(s, rows, D, V, x, w, bias, labels, blocks, st);
   if (rc != LP_OK) return rc;
   LP_CUDA_OK(launch_pdl(ce_finish_kernel, dim3(1), dim3(1024), 0, st, (const float2*)s.stats, (long long)s.rows, blocks, rows, V, labels,
-                        (const float*)s.target, s.lse, row_loss, loss));
+                        s.target, s.top, row_loss, loss));
   return LP_OK;
 }
 template <typename T, int kRows>
@@ -482,17 +482,17 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
     const bool finished = rows == T && rows <= 64 && parts <= 128;
     if (finished)
       LP_CUDA_OK(launch_pdl(ce_finish_kernel, dim3(1), dim3(1024), 0, st, (const float2*)s.stats, (long long)s.rows, parts, rows, V, labels,
-                            (const float*)s.target, s.lse, rl, loss_out));
+                            s.target, s.top, rl, loss_out));
     else
       LP_CUDA_OK(launch_pdl(ce_rows_kernel, dim3((rows + 7) / 8), dim3(kCeThreads), 0, st, (const float2*)s.stats, (long long)s.rows, parts,
-                            r0, rows, T, V, labels, (const float*)s.target, s.lse, rl, s.hdr, r0 + rows == T ? loss_out : nullptr));
+                            r0, rows, T, V, labels, s.target, s.top, rl, s.hdr, r0 + rows == T ? loss_out : nullptr));
     if (!grads) continue;
     const int slabs = (rows + kCeSlab - 1) / kCeSlab;
     one_slab = slabs == 1 && rows == T;
     float* sums = dbias && !one_slab ? s.sums + (long long)slab0 * V : nullptr;
     LP_CUDA_OK(launch_pdl(s.f32 ? ce_dl_kernel<true> : ce_dl_kernel<false>, dim3((V + 255) / 256, slabs), dim3(kCeThreads), 0, st, s.p, s.ld_v,
-                          p_plane, rows, V, (const float2*)s.stats, (long long)s.rows, part_cols, (const float*)(s.lse + r0),
-                          (const float*)(s.target + r0), labels + r0, sums, one_slab ? dbias : nullptr, (const CeHeader*)s.hdr));
+                          p_plane, rows, V, (const float2*)s.stats, (long long)s.rows, part_cols, (const float*)(s.top + r0),
+                          (const float*)(s.target + r0), (const float*)(rl + r0), labels + r0, sums, one_slab ? dbias : nullptr, (const CeHeader*)s.hdr));
     slab0 += slabs;
     bool dx_idle = false;
     const GemmOperand op{s.p, V, rows, s.ld_v, p_plane, planes, !s.f32};

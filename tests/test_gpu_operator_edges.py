@@ -2,7 +2,7 @@
 masked classes), where logits are far from 0, and at the precision that include/lp.h states."""
 import pytest
 
-from test_gpu_operators import EPS32, ce_check, ce_inputs, ce_reference, ce_run, muon_reference, ortho_reference, ortho_run, \
+from test_gpu_operators import EPS32, EPSB, ce_check, ce_inputs, ce_reference, ce_run, muon_reference, ortho_reference, ortho_run, \
     ortho_tol, rel, scratch_of, spectrum
 
 pytestmark = pytest.mark.gpu
@@ -276,3 +276,42 @@ def test_gradients_in_fp32_are_as_exact_as_stated(size):
     got, ref = ce_run(x, w, b, labels), ce_reference(x, w, b, labels)
     for k in ("dx", "dw"):
         assert rel(got[k], ref[k]) < 1e-6, k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 64, 300), (20, 64, 700), (65, 200, 5003), (300, 64, 700), (700, 264, 20011)], ids=str)
+@pytest.mark.parametrize("lift", [0.0, 2000.0])
+def test_confident_rows_keep_their_small_losses(size, lift, dtype):
+    """Rows whose label's logit is the largest by 2 to 20 or so, all logits `lift` higher.  Logits off by e move such a row's loss by
+    2 e (1 - p) <= 2 e row_loss, and what is left is the statistics' own error, whatever the logits: the sum of exponentials from
+    1 on is off by 2^-24 at most for each term that is added to the largest, 32 in a part of 128 columns (four chains), 2 where
+    the chains meet, up to 20 parts a lane and 5 exchanges between lanes, and its logarithm by a few more: 64.  dl: the label's the
+    same; the others' a product of probabilities off by 2 e each (LP_BF16: fp16 exponentials and one
+    rounding to bf16)."""
+    import torch
+    T, D, V = size
+    f32 = dtype == "f32"
+    x, w, b, labels = ce_inputs(T, D, V, dtype, seed=17)
+    gen = torch.Generator("cuda").manual_seed(18)
+    y = labels.long()
+    gap = 2 + 18 * torch.rand(T, generator=gen, device="cuda", dtype=torch.float64)
+    for _ in range(6):      # along the label's weights until its logit is the largest by `gap`
+        l = x.double() @ w.double().T + b.double()
+        at = l.gather(1, y[:, None])[:, 0]
+        top = l.scatter(1, y[:, None], float("-inf")).amax(1)
+        x = (x.double() + ((top + gap - at) / (w.double()[y] ** 2).sum(1))[:, None] * w.double()[y]).to(x.dtype)
+    b = (b.double() + lift).to(b.dtype)
+    ref, got, alone = ce_reference(x, w, b, labels), ce_run(x, w, b, labels), ce_run(x, w, b, labels, grads=False)
+    assert float(ref["row_loss"].median()) < 1e-2
+    acc = lambda K: ((48 + K / 256) if f32 else K / 16 + 4) * 2 * EPS32  # noqa: E731  (as in ce_check)
+    rep = 3 * 2.0 ** -22 if f32 else 0.0
+    e_l = (rep + acc(D)) * ref["mag_l"].amax(1) + 8 * EPS32 * ref["l"].abs().amax(1)
+    tol = 2 * e_l * ref["row_loss"] + 64 * EPS32
+    for r in (got, alone):
+        assert bool(((r["row_loss"].double() - ref["row_loss"]).abs() <= tol).all())
+    p1 = ref["d"].abs()
+    e_d = 2 * e_l[:, None] * p1 + (4 * 2.0 ** -22 * p1 + 2.0 ** -38 if f32 else (EPSB + 2.0 ** -10) * p1 + 2.0 ** -24)
+    e_d = e_d.scatter_add(1, y[:, None], torch.full((T, 1), 64 * EPS32, dtype=torch.float64, device="cuda"))
+    aw = ref["w"].abs()
+    tol = abs(ref["g"]) * (e_d @ aw + (rep + acc(V)) * (p1 @ aw)) + 2 * (EPS32 if f32 else EPSB) * ref["dx"].abs() + 1e-30
+    assert bool(((got["dx"].double() - ref["dx"]).abs() <= tol).all())
