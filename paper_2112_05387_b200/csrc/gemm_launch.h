@@ -91,7 +91,7 @@ static unsigned rows_b(const GemmCut& cut) { return cut.kind == tc::GEMM_HALF ? 
 // cycles a load (64 bytes a cycle from L2) or, for each product, 512 cycles (128 x 256 of a pair's tile; 690 with one plane of
 // each operand, measured: 0.47 us with 42 pairs at work) or 256 (128 x 128).  Half a pair's tile, 256 x 128, has three products of
 // 256 cycles and loads of as many (128 rows of A and 64 of B in two parts, 48 KB): what the last wave leaves idle is halved (fp32
-// loss of 1001 x 640 x 20011 332 -> 310 us, 2 x 2048 x 512 196 -> 191); with one product a K block its loads would take 1.5 times
+// loss of 1001 x 640 x 20011 in rounds of four K blocks 332 -> 310 us, 2 x 2048 x 512 196 -> 191); with one product a K block its loads would take 1.5 times
 // as long as the product.  With few tiles a cluster shares K, at the price of an exchange: about 2500 cycles beside three products
 // a K block, 4500 beside one or two, whose K blocks take less than counted here while few SMs draw on L2 (us a call of five steps
 // with 800, 2000, 3000, 4500, 6500 cycles: 300 x 400 in fp32 130, 130, 131, 145, 161, 600 x 600 in bf16 126, 126, 126, 115, 116,

@@ -518,7 +518,7 @@ int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const
       p.a_planes = p.b_planes = planes;
       p.f = 1.f; p.f_dev = &s.hdr->dw_f; p.f_pow = 1;
       p.out = dw; p.out_bf16 = is_bf16; p.out_ld = D;
-      // (beside dx's product where that leaves SMs idle: 64 rows x 512 x 1000 30 us and 33 one after the other, fp32 43 and 48;
+      // (beside dx's product where that leaves SMs idle: 64 rows x 512 x 1000 28.5 us and 30.5 one after the other, fp32 39.5 and 45;
       // where it has all of them the two share L2 badly, 4096 x 2048 x 32000 1.32 ms and 1.31)
       p.wait_late = dx_idle ? &s.hdr->dl_seen : nullptr; p.turn = r0 / s.rows + 1;
       if (s.rows < T) {
