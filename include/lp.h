@@ -402,7 +402,7 @@ int lp_conv2d_fwd_noalloc(int N, int H, int W, int Cin, int Cout, int R, int str
  * Scratch: a piece is as many rows as have 512 MB of exponentials, 256 at least and 2^18 at most, or in LP_BF16 all rows where
  * their exponentials take no more than 4 V D bytes, the fp32 sums of dw that several pieces need.  Beside it stand x (and w, in
  * LP_F32 or where D is no multiple of 8) in 16-bit parts, up to 8 bytes for each row of a piece and 32 classes, and, for
- * gradients, 4 bytes for each class and 64 rows. */
+ * gradients, 4 bytes for each class and 64 rows.  What is asked for with gradients is enough for the loss alone, too. */
 size_t lp_linear_cross_entropy_scratch_bytes(int dtype, int T, int D, int V, int grads);
 int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const void* w, const void* bias,
                             const int32_t* labels, float grad_scale, float* loss_out, float* row_loss, void* dx, void* dw,

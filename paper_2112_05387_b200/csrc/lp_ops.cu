@@ -411,9 +411,11 @@ static bool ce_size_ok(int T, int D, int V) {
 
 size_t lp_linear_cross_entropy_scratch_bytes(int dtype, int T, int D, int V, int grads) {
   if ((dtype != LP_F32 && dtype != LP_BF16) || !ce_size_ok(T, D, V)) return 0;
-  Carve c{nullptr};
-  ce_carve(c, dtype, T, D, V, grads != 0);
-  return c.off;
+  // (what the gradients need is enough for the loss alone: one scratch serves training and evaluation)
+  Carve alone{nullptr}, c{nullptr};
+  ce_carve(alone, dtype, T, D, V, false);
+  if (grads) ce_carve(c, dtype, T, D, V, true);
+  return std::max(alone.off, c.off);
 }
 
 int lp_linear_cross_entropy(int dtype, int T, int D, int V, const void* x, const void* w, const void* bias, const int32_t* labels,

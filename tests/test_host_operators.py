@@ -101,6 +101,15 @@ def test_scratch_of_few_classes_goes_by_the_classes():
             assert 0 < lp.lp_linear_cross_entropy_scratch_bytes(dtype, T, D, V, True) <= with_grads
 
 
+@pytest.mark.parametrize("dtype", [lp.LP_F32, lp.LP_BF16])
+def test_scratch_of_the_gradients_is_enough_for_the_loss_alone(dtype):
+    for T in (1, 4, 5, 300, 70000, 1 << 20):
+        for D in (1, 72, 4096):
+            for V in (1, 5, 1000, 130000, 1 << 22):
+                alone, both = [lp.lp_linear_cross_entropy_scratch_bytes(dtype, T, D, V, grads) for grads in (False, True)]
+                assert 0 < alone <= both, (T, D, V)
+
+
 def test_step_and_status_need_a_handle_and_a_scratch():
     lib = lp.library()
     assert lib.lp_step_muon_scratch_bytes(None) == 0
